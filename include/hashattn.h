@@ -60,7 +60,7 @@ extern "C" {
 /* bits of the device status word (ha_read_device_status) */
 #define HA_DEV_BAD_INDEX 1u /* an idx entry >= seq_len was met and skipped */
 #define HA_DEV_TIMEOUT 2u   /* a bounded wait inside a kernel gave up (ha_encode_prefill's tensor-core path,
-                               ha_sparse_decode_pipelined); the kernel returned early and its outputs are not valid */
+                               ha_sparse_decode_pipelined, ha_chunk_attn_paged); the kernel returned early and its outputs are not valid */
 
 #define HA_HEAD_DIM 128
 #define HA_N_BITS 32
@@ -361,6 +361,33 @@ int ha_sparse_decode_paged_codes(const ha_shape *shape, const ha_mapping *map_q,
                                  const int32_t *k_per_seq, int32_t k_uniform, int32_t max_seq_len, int32_t k_max,
                                  uint32_t *q_codes, int32_t *idx, int64_t idx_stride_b, int64_t idx_stride_h, int32_t *count,
                                  uint16_t *out, float *lse, void *workspace, size_t ws_bytes, void *stream);
+
+/* Exact attention of NEW tokens over the paged cache: a chunk of each prompt on its way into the cache, or the one new token
+ * of a decoding sequence where nothing is to be left out (the method starts from full attention, Section 3.1; its sparse step
+ * takes over once a prompt is cached).  Sequence b brings the rows q_offsets[b] .. q_offsets[b + 1] - 1 of q (packed, no padding;
+ * any number, none included) and has seq_lens[b] tokens in the cache, its new ones among them as the last: row i of its n new
+ * ones is the query of token seq_lens[b] - n + i and attends to that token and all before it (causal != 0) or to all
+ * seq_lens[b] tokens (causal == 0):
+ *     out = sum_t softmax_t(sm_scale <q, k_t>) v_t,   lse = log sum_t exp(sm_scale <q, k_t>).
+ * fp32 accumulation; softmax weights enter the product with V as bf16; one rounding of out to bf16.  A row that sees no token
+ * (more new tokens than cached ones) gives out = 0, lse = -inf.  Rows of q and out outside the sequences' ranges are neither
+ * read nor written.  Tokens at or beyond seq_lens[b], and what lies in unused slots of a page, do not matter, NaN or not.
+ *   q            bf16 rows [n_rows][n_q_heads][128]: stride_n steps over tokens, stride_h over heads (stride_b is not used; heads
+ *                may overlap other data, as in one projection output that holds q, k and v), multiples of 8
+ *   q_offsets    i32 [batch + 1], ascending, within 0 .. n_rows (device); a sequence with bad ones is left out and raises
+ *                HA_DEV_BAD_INDEX
+ *   K_pool, V_pool, block_table, page_size   as in ha_gather_attn_paged; n_pages bounds the page numbers: tokens on a page outside
+ *                0 .. n_pages - 1 read as zeros and raise HA_DEV_BAD_INDEX (the sequence's output is then of no use)
+ *   out          bf16 [n_rows][n_q_heads][128] contiguous; lse fp32 [n_rows][n_q_heads] or NULL
+ *   workspace    ha_workspace_bytes_chunk() bytes, the same for all shapes; prepared once with ha_workspace_init
+ * n_sink / n_local of the shape are not looked at.  Results do not depend on how the work is split: the same call gives the same
+ * bits.  If a wait inside the kernel runs out (it never should) it raises HA_DEV_TIMEOUT and out must not be used; call
+ * ha_workspace_init before the workspace is used again. */
+size_t ha_workspace_bytes_chunk(void);
+int ha_chunk_attn_paged(const ha_shape *shape, const ha_tensor *q, const int32_t *q_offsets, int32_t n_rows,
+                        const ha_tensor *K_pool, const ha_tensor *V_pool, int32_t n_pages, const int32_t *block_table,
+                        int64_t bt_stride_b, int32_t page_size, const int32_t *seq_lens, int32_t causal, uint16_t *out,
+                        float *lse, void *workspace, size_t ws_bytes, void *stream);
 
 /* GATHER-ATT without a caller-provided workspace.  (The paper has no counterpart of this entry
  * point; it exists for integration reasons only.)

@@ -31,6 +31,7 @@ EXPORTS = [
     "ha_encode_wide", "ha_workspace_bytes_wide", "ha_score_topk_wide",
     "ha_score_topk_paged", "ha_score_topk_per_head_paged", "ha_gather_attn_per_head_paged", "ha_encode_append_paged",
     "ha_sparse_decode_paged_codes",
+    "ha_workspace_bytes_chunk", "ha_chunk_attn_paged",
     "ha_kernel_launches", "ha_status_string", "ha_version",
 ]
 
@@ -108,6 +109,9 @@ def lib() -> C.CDLL:
         L.ha_workspace_bytes_wide.argtypes = [P, I32]
         L.ha_score_topk_wide.argtypes = [P, I32, P, P, I64, I64, P, P, I32, I32, I32, P, I64, I64, P, P, P, SZ, P]
         L.ha_score_topk_wide.restype = C.c_int
+        L.ha_workspace_bytes_chunk.restype = SZ
+        L.ha_chunk_attn_paged.argtypes = [P, P, P, I32, P, P, I32, P, I64, I32, P, I32, P, P, P, SZ, P]
+        L.ha_chunk_attn_paged.restype = C.c_int
         L.ha_inner_products.argtypes = [P, P, I64, I64, P, P]
         L.ha_kernel_launches.restype = C.c_uint64
         L.ha_status_string.restype = C.c_char_p
@@ -377,6 +381,26 @@ def ha_sparse_decode_paged_codes(shape: ha_shape, map_q: Mapping, map_k: Optiona
     _check("ha_sparse_decode_paged_codes", _host().sparse_decode_paged_codes(
         shape, map_q, map_k, q, k_new, K_pool, V_pool, code_pool, block_table, seq_lens, k_per_seq, k_uniform, max_seq_len, k_max,
         q_codes, idx, count, out, workspace, lse, stream))
+
+
+def ha_workspace_bytes_chunk() -> int:
+    return int(lib().ha_workspace_bytes_chunk())
+
+
+def alloc_workspace_chunk(device="cuda") -> torch.Tensor:
+    """A workspace for ha_chunk_attn_paged, initialised; one size serves every shape."""
+    ws = torch.empty(ha_workspace_bytes_chunk(), dtype=torch.uint8, device=device)
+    ha_workspace_init(ws)
+    return ws
+
+
+def ha_chunk_attn_paged(shape: ha_shape, q, q_offsets, K_pool, V_pool, block_table, page_size: int, seq_lens, out, workspace,
+                        lse=None, causal: bool = True, stream=None) -> None:
+    """Exact attention of new tokens over the paged cache: q bf16 [rows, Hq, 128] packed by q_offsets int32 [B + 1]; pools bf16
+    [n_pages, Hkv, page_size, 128]; block_table int32 [B, pages]; seq_lens int32 [B], new tokens among them; out bf16
+    [rows, Hq, 128]; lse fp32 [rows, Hq]."""
+    _check("ha_chunk_attn_paged", _host().chunk_attn_paged(shape, q, q_offsets, K_pool, V_pool, block_table, page_size, seq_lens, out,
+                                                           workspace, lse, 1 if causal else 0, stream))
 
 
 def ha_gather_attn_static(shape: ha_shape, q, K, V, seq_lens, idx, count, k_max: int, out, lse=None, stream=None) -> None:

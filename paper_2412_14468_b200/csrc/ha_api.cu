@@ -561,6 +561,48 @@ int ha_sparse_decode_paged_codes(const ha_shape *shape, const ha_mapping *map_q,
                               out, lse, workspace, ws_bytes, stream, nullptr, false, cp);
 }
 
+// ---- new tokens over a paged cache
+
+// Pools of K and V rows in pages: a page is page_size consecutive slots, both pools step through pages in whole rows alike.
+static int check_paged_kv(const ha_tensor *K_pool, const ha_tensor *V_pool, int32_t n_pages, const int32_t *block_table,
+                          int32_t page_size, int *shift) {
+    HA_TRY(check_tensor(K_pool));
+    HA_TRY(check_tensor(V_pool));
+    if (!block_table || n_pages < 0) return HA_ERR_INVALID_ARG;
+    if (page_size <= 0 || (page_size & (page_size - 1)) || page_size > 65536) return HA_ERR_INVALID_ARG;
+    if (K_pool->stride_b % K_pool->stride_n != 0 || V_pool->stride_b % V_pool->stride_n != 0 ||
+        K_pool->stride_b / K_pool->stride_n != V_pool->stride_b / V_pool->stride_n)
+        return HA_ERR_INVALID_ARG;
+    *shift = 0;
+    while ((1 << *shift) < page_size) ++*shift;
+    return HA_OK;
+}
+// Packed rows [n_rows][heads][128]: both strides multiples of 8 elements, heads of a row apart from one another.
+static int check_rows(const ha_tensor *t) {
+    if (!t || !t->ptr) return HA_ERR_INVALID_ARG;
+    if (((uintptr_t)t->ptr & 15) || (t->stride_h & 7) || (t->stride_n & 7) || t->stride_h < kD || t->stride_n < 0) return HA_ERR_INVALID_ARG;
+    return HA_OK;
+}
+
+size_t ha_workspace_bytes_chunk(void) { return chunk_workspace_bytes(); }
+
+int ha_chunk_attn_paged(const ha_shape *shape, const ha_tensor *q, const int32_t *q_offsets, int32_t n_rows, const ha_tensor *K_pool,
+                        const ha_tensor *V_pool, int32_t n_pages, const int32_t *block_table, int64_t bt_stride_b, int32_t page_size,
+                        const int32_t *seq_lens, int32_t causal, uint16_t *out, float *lse, void *workspace, size_t ws_bytes,
+                        void *stream) {
+    HA_TRY(check_shape(shape));
+    HA_TRY(check_rows(q));
+    int shift;
+    HA_TRY(check_paged_kv(K_pool, V_pool, n_pages, block_table, page_size, &shift));
+    if (!q_offsets || !seq_lens || !out || n_rows < 0 || ((uintptr_t)out & 15)) return HA_ERR_INVALID_ARG;
+    if (!workspace || ((uintptr_t)workspace & 255) || ws_bytes < chunk_workspace_bytes()) return HA_ERR_WORKSPACE;
+    if (shape->batch == 0 || n_rows == 0) return HA_OK;
+    HA_CUDA(launch_chunk_attn(shape->batch, shape->n_q_heads, shape->n_kv_heads, shape->sm_scale, view(q), q_offsets, n_rows,
+                              view(K_pool), view(V_pool), n_pages, block_table, bt_stride_b, shift, seq_lens, causal != 0, out, lse,
+                              workspace, (cudaStream_t)stream));
+    return HA_OK;
+}
+
 // Both host-buffer entries: block_table == NULL is the contiguous cache, else K / V are pools (page_shift = log2 of
 // the page size).
 static int sparse_decode_host_impl(const ha_shape *shape, const ha_mapping *map_q, const ha_mapping *map_k,

@@ -1,0 +1,623 @@
+// Attention of new tokens over a paged cache: every new token (one of a decoding sequence, or a chunk of a prompt) attends to all
+// cached tokens up to its own, exactly.
+//
+//     out_i = sum_{t <= pos_i} softmax_t(scale <q_i, k_t>) v_t,   pos_i = seq_len - n_new + i
+//
+// One pass over the keys with a running maximum m and sum l per row: p = 2^(s - m) in 32 bits, l += p, O += bf16(p) V; the maximum
+// that the exponents refer to is raised, and O and l rescaled, only when a tile's maximum lies more than 2^8 above it, so that most
+// tiles leave O alone (p <= 2^8: sums stay far inside 32 bits).  p is rounded to bf16 for the tensor cores, as V is bf16 and both
+// operands have one type: half a step, 2^-9 relative, on each weight, of independent sign; l sums the unrounded p.
+//
+// Work: see ha_chunk_plan.h.  A CTA holds two tiles of 128 query rows (tokens x heads of a group, so that one fetch of K and V
+// serves the whole group) and streams key tiles of 128 tokens through a ring in shared memory.  Tensor memory: O of both row tiles
+// and S of both, 128 columns each; P (bf16) overwrites the first half of the S that it comes from.
+//   warps 0 - 3, 4 - 7   softmax of row tile 0 / 1: one thread per row
+//   warp 8               issues the MMAs: S = Q K^T (K-major operands), O += P V (P from tensor memory, V N-major)
+//   warps 9 - 11         copy Q, K and V rows into the 128-byte swizzle, through the block table
+// While one row tile is in its softmax the tensor cores work for the other.  A unit of at most 128 rows (a decoding sequence) uses
+// the same two halves for alternate key tiles and joins them at its end.
+// A unit cut between CTAs: each part writes m, l and O to the workspace; the part that arrives last joins them all, in the order of
+// the keys, so that results do not depend on the order of arrival.
+// Every wait is bounded: a waiter that gives up raises HA_DEV_TIMEOUT, all roles stop, the MMAs in flight are waited for and the
+// tensor memory is given back.
+#include "ha_attn_dev.cuh"
+#include "ha_chunk_plan.h"
+#include "ha_encode_dev.cuh"
+#include "ha_umma.cuh"
+
+namespace ha {
+
+constexpr int kC_Softmax = 256;                    // threads of the softmax roles
+constexpr int kC_Mma = kC_Softmax / 32;            // the issuing warp
+constexpr int kC_Load = 96;                        // threads that copy (12 warps in all: 168 registers a thread)
+constexpr int kC_Threads = kC_Softmax + 32 + kC_Load;
+constexpr int kC_TileBytes = kChunkTile * kD * 2;  // 32768: two halves of 64 columns, each 128 rows of 128 bytes
+constexpr int kC_Half = kC_TileBytes / 2;
+constexpr int kC_Stages = 5;                       // ring of K and V tiles
+constexpr int kC_OffQ = 0, kC_OffRing = 2 * kC_TileBytes;
+constexpr int kC_Smem = kC_OffRing + kC_Stages * kC_TileBytes;   // 229376
+constexpr int kC_Ahead = 3;                        // tiles whose copies are in flight before the oldest is waited for
+constexpr float kC_Raise = 8.0f;                   // how far (log2) a maximum may lie above the one that is referred to
+constexpr uint32_t kC_ColS = 256, kC_ColO = 0;     // tensor-memory columns: O0, O1, S0, S1
+
+struct ChunkArgs {
+    const uint16_t *q;
+    long long q_sn, q_sh;
+    const int32_t *offsets, *seq_lens, *table;
+    TensorView K, V;
+    long long bt_sb;
+    int n_rows, n_pages, shift, B, Hkv, log2g, causal, max_ctas;
+    float scale_log2;
+    uint16_t *out;
+    float *lse;
+    uint32_t *status;
+    int32_t *tickets;
+    float *part_ml, *part_acc;   // [CTA][2][256] (m, l) and [CTA][2][256][128]
+};
+
+struct ChunkShared {
+    unsigned long long kv_full[kC_Stages], kv_empty[kC_Stages], q_full, q_empty, s_full[2], p_full[2], o_full[2], joint, drained;
+    long long start_rest, total;
+    long long warp_sums[kC_Threads / 32];
+    int start_b;
+    int last_part;
+    uint32_t tmem;
+    volatile int fail;
+    float ml[2][128][2];         // the halves' maxima and sums, where they share a unit
+};
+
+__device__ __forceinline__ float exp2_approx(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+__global__ void __launch_bounds__(kC_Threads, 1) chunk_attn_kernel(const ChunkArgs a) {
+    extern __shared__ __align__(1024) unsigned char smem[];
+    __shared__ __align__(8) ChunkShared sh;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const uint32_t smem0 = smem_u32(smem);
+
+    if (tid == 0) {
+        for (int i = 0; i < kC_Stages; ++i) {
+            mbar_init(smem_u32(&sh.kv_full[i]), kC_Load);
+            mbar_init(smem_u32(&sh.kv_empty[i]), 1);
+        }
+        mbar_init(smem_u32(&sh.q_full), kC_Load);
+        mbar_init(smem_u32(&sh.q_empty), 1);
+        for (int x = 0; x < 2; ++x) {
+            mbar_init(smem_u32(&sh.s_full[x]), 1);
+            mbar_init(smem_u32(&sh.p_full[x]), 4);
+            mbar_init(smem_u32(&sh.o_full[x]), 1);
+        }
+        mbar_init(smem_u32(&sh.joint), kC_Softmax / 32);
+        mbar_init(smem_u32(&sh.drained), 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        sh.fail = 0;
+        sh.start_b = -1;
+    }
+    pdl_wait();
+    pdl_launch_dependents();   // nothing that a kernel reads before its own wait is written here or by anything still running
+    if (warp == 0) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh.tmem)), "r"(512u) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+
+    // ---- the whole work, and where this CTA's share of it begins
+    auto cost_of = [&](int b, bool report) -> long long {
+        if (b >= a.B) return 0;
+        bool bad;
+        const ChunkSeq s = chunk_seq(a.seq_lens[b], a.offsets[b], a.offsets[b + 1], a.n_rows, a.log2g, bad);
+        if (bad && report && a.status) atomicOr(a.status, HA_DEV_BAD_INDEX);
+        return a.Hkv * chunk_cost_head(s, a.log2g, a.causal);
+    };
+    // sum over the block and, in `before`, over the threads in front of this one
+    auto block_sum = [&](long long v, long long &before) -> long long {
+        long long x = v;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const long long y = __shfl_up_sync(0xffffffffu, x, d);
+            if (lane >= d) x += y;
+        }
+        __syncthreads();
+        if (lane == 31) sh.warp_sums[warp] = x;
+        __syncthreads();
+        long long base = 0, all = 0;
+        for (int w = 0; w < kC_Threads / 32; ++w) {
+            if (w < warp) base += sh.warp_sums[w];
+            all += sh.warp_sums[w];
+        }
+        before = base + x - v;
+        return all;
+    };
+    long long W = 0, before = 0, mine = 0;
+    for (int b0 = 0; b0 < a.B; b0 += kC_Threads) {
+        mine = cost_of(b0 + tid, blockIdx.x == 0);
+        W += block_sum(mine, before);
+    }
+    const int C = chunk_ctas(W, a.max_ctas < (int)gridDim.x ? a.max_ctas : (int)gridDim.x);
+    const bool busy = W > 0 && (int)blockIdx.x < C;
+    if (busy) {
+        const long long f0 = chunk_bound(W, C, blockIdx.x);
+        long long done = 0;
+        for (int b0 = 0; b0 < a.B; b0 += kC_Threads) {
+            long long all = W;
+            if (a.B > kC_Threads) {
+                mine = cost_of(b0 + tid, false);
+                all = block_sum(mine, before);
+            }
+            const long long first = done + before;
+            if (first <= f0 && f0 < first + mine) {
+                sh.start_b = b0 + tid;
+                sh.start_rest = f0 - first;
+            }
+            done += all;
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = sh.tmem;
+
+    auto wait = [&](unsigned long long &bar, uint32_t parity) -> bool {
+        const uint32_t at = smem_u32(&bar);
+        if (mbar_test(at, parity)) return true;
+        if (!mbar_wait_parity(at, parity)) {
+            sh.fail = 1;
+            if (a.status) atomicOr(a.status, HA_DEV_TIMEOUT);
+            return false;
+        }
+        return sh.fail == 0;
+    };
+
+    if (busy && sh.start_b >= 0) {
+        ChunkWalk walk;
+        walk.W = W; walk.C = C; walk.log2g = a.log2g; walk.B = a.B; walk.Hkv = a.Hkv; walk.n_rows = a.n_rows; walk.causal = a.causal != 0;
+        walk.seq_lens = a.seq_lens; walk.offsets = a.offsets;
+        walk.begin(blockIdx.x, sh.start_b, sh.start_rest);
+
+        if (warp > kC_Mma) {
+            // ------------------------------------------------ copies
+            const int p = tid - kC_Softmax - 32, pw = p >> 5, hw = lane >> 4, ch = lane & 15;
+            const uint32_t piece = (uint32_t)(ch >> 3) * kC_Half;
+            int stage = 0, pending = 0, oldest = 0;   // copies of `pending` tiles are not announced yet, the first in ring slot `oldest`
+            uint32_t phase = 1;                       // of kv_empty: the ring starts empty
+            auto announce = [&]() {                   // the oldest tile has landed for this thread
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                mbar_arrive(smem_u32(&sh.kv_full[oldest]));
+                oldest = oldest + 1 == kC_Stages ? 0 : oldest + 1;
+                --pending;
+            };
+            auto flush = [&]() {
+                cp_async_wait<0>();
+                while (pending > 0) announce();
+            };
+            // rows of key tile j of the part, K or V: every warp looks up all 128 pages, half-warps copy rows
+            auto load = [&](const TensorView &T, int j) -> bool {
+                long long off[4];
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const int tok = j * kChunkTile + g * 32 + lane;
+                    off[g] = -1;
+                    if (tok < walk.s.n) {
+                        const int page = __ldg(a.table + (long long)walk.b * a.bt_sb + (tok >> a.shift));
+                        if ((unsigned)page < (unsigned)a.n_pages)
+                            off[g] = (long long)page * T.sb + (long long)walk.h * T.sh + (long long)(tok & ((1 << a.shift) - 1)) * T.sn;
+                        else if (a.status) atomicOr(a.status, HA_DEV_BAD_INDEX);
+                    }
+                }
+                if (!mbar_test(smem_u32(&sh.kv_empty[stage]), phase)) {
+                    flush();   // what is waited for may wait for these tiles
+                    if (!wait(sh.kv_empty[stage], phase)) return false;
+                }
+                const uint32_t dst = smem0 + kC_OffRing + stage * kC_TileBytes + piece;
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    for (int i = (pw + 3 - (g * 16) % 3) % 3; i < 16; i += 3) {
+                        const int lr = 2 * i + hw, r = g * 32 + lr;
+                        const long long o = __shfl_sync(0xffffffffu, off[g], lr);
+                        cp_async16(dst + r * 128 + (((ch & 7) ^ (r & 7)) << 4),
+                                   reinterpret_cast<const unsigned char *>(T.ptr + (o >= 0 ? o : 0)) + ch * 16, o >= 0 ? 16u : 0u);
+                    }
+                }
+                cp_async_commit();
+                if (++stage == kC_Stages) { stage = 0; phase ^= 1; }
+                if (++pending > kC_Ahead) {
+                    cp_async_wait<kC_Ahead>();
+                    announce();
+                }
+                return true;
+            };
+            bool ok = true;
+            for (uint32_t part = 0; ok && walk.next(); ++part) {
+                flush();
+                if (part > 0 && !wait(sh.q_empty, (part - 1) & 1u)) break;
+                const int n_rows = walk.unit.toks << a.log2g;
+                const int rows = n_rows <= 128 ? 128 : 256;
+                const uint16_t *q = a.q + (long long)(walk.s.row0 + walk.unit.tok0) * a.q_sn + (long long)(walk.h << a.log2g) * a.q_sh;
+                for (int r = pw * 2 + hw; r < rows; r += kC_Load / 16) {
+                    const bool in = r < n_rows;
+                    const uint16_t *src = in ? q + (long long)(r >> a.log2g) * a.q_sn + (long long)(r & ((1 << a.log2g) - 1)) * a.q_sh : q;
+                    cp_async16(smem0 + kC_OffQ + (r >> 7) * kC_TileBytes + piece + (r & 127) * 128 + (((ch & 7) ^ (r & 7)) << 4),
+                               reinterpret_cast<const unsigned char *>(src) + ch * 16, in ? 16u : 0u);
+                }
+                cp_async_commit();
+                cp_async_wait<0>();
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                mbar_arrive(smem_u32(&sh.q_full));
+                const int t0 = walk.t0, t1 = walk.t1;
+                // the order in which the issuing warp waits for them
+                const int lead = walk.unit.split ? 2 : 1;
+                for (int j = t0; ok && j < t0 + lead && j < t1; ++j) ok = load(a.K, j);
+                for (int j = t0; ok && j < t1; ++j) {
+                    ok = load(a.V, j);
+                    if (ok && j + lead < t1) ok = load(a.K, j + lead);
+                }
+            }
+            flush();
+        } else if (warp == kC_Mma) {
+            // ------------------------------------------------ MMAs
+            constexpr uint32_t kIdescS = umma_idesc(128, 128, false), kIdescO = umma_idesc(128, 128, true);
+            const uint32_t base = __shfl_sync(0xffffffffu, tmem, 0);
+            int stage = 0;
+            uint32_t phase = 0, p_phase[2] = {0, 0};
+            auto step = [&]() { if (++stage == kC_Stages) { stage = 0; phase ^= 1; } };
+            auto s_mma = [&](int qx, int x, int at) {   // S_x = Q_qx K^T
+                const uint64_t qd = umma_desc_sw128(smem0 + kC_OffQ + qx * kC_TileBytes, 16, 1024);
+                const uint64_t kd = umma_desc_sw128(smem0 + kC_OffRing + at * kC_TileBytes, 16, 1024);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const uint64_t d = (uint64_t)((i >> 2) * (kC_Half >> 4) + (i & 3) * 2);
+                    umma_ss(base + kC_ColS + x * 128, qd + d, kd + d, kIdescS, i ? 1u : 0u);
+                }
+                umma_commit(smem_u32(&sh.s_full[x]));
+            };
+            auto o_mma = [&](int x, int at, bool add) {   // O_x += P_x V
+                const uint64_t vd = umma_desc_sw128(smem0 + kC_OffRing + at * kC_TileBytes, kC_Half, 1024);
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    umma_ts(base + kC_ColO + x * 128, base + kC_ColS + x * 128 + i * 8, vd + (uint64_t)(i * (2048 >> 4)), kIdescO, (add || i) ? 1u : 0u);
+            };
+            bool ok = true;
+            for (uint32_t part = 0; ok && walk.next(); ++part) {
+                const int n = walk.t1 - walk.t0;
+                if (!(ok = wait(sh.q_full, part & 1u))) break;
+                if (walk.unit.split) {
+                    for (int j = 0; ok && j < 2 && j < n; ++j) {
+                        if (!(ok = wait(sh.kv_full[stage], phase))) break;
+                        tc_fence_after();
+                        if (elect_one()) {
+                            s_mma(0, j, stage);
+                            umma_commit(smem_u32(&sh.kv_empty[stage]));
+                        }
+                        __syncwarp();
+                        step();
+                    }
+                    for (int j = 0; ok && j < n; ++j) {
+                        const int x = j & 1;
+                        ok = wait(sh.kv_full[stage], phase) && wait(sh.p_full[x], p_phase[x]);
+                        if (!ok) break;
+                        p_phase[x] ^= 1;
+                        tc_fence_after();
+                        if (elect_one()) {
+                            o_mma(x, stage, j >= 2);
+                            umma_commit(smem_u32(&sh.kv_empty[stage]));
+                        }
+                        __syncwarp();
+                        step();
+                        if (j + 2 < n) {
+                            if (!(ok = wait(sh.kv_full[stage], phase))) break;
+                            tc_fence_after();
+                            if (elect_one()) {
+                                s_mma(0, x, stage);
+                                umma_commit(smem_u32(&sh.kv_empty[stage]));
+                            }
+                            __syncwarp();
+                            step();
+                        }
+                    }
+                } else {
+                    if (!(ok = wait(sh.kv_full[stage], phase))) break;
+                    tc_fence_after();
+                    if (elect_one()) {
+                        s_mma(0, 0, stage);
+                        s_mma(1, 1, stage);
+                        umma_commit(smem_u32(&sh.kv_empty[stage]));
+                    }
+                    __syncwarp();
+                    step();
+                    for (int j = 0; ok && j < n; ++j) {
+                        const int v = stage;
+                        ok = wait(sh.kv_full[v], phase);
+                        step();
+                        const bool more = j + 1 < n;
+                        for (int x = 0; ok && x < 2; ++x) {
+                            if (!(ok = wait(sh.p_full[x], p_phase[x]))) break;
+                            p_phase[x] ^= 1;
+                            tc_fence_after();
+                            if (elect_one()) {
+                                o_mma(x, v, j > 0);
+                                if (x == 1) umma_commit(smem_u32(&sh.kv_empty[v]));
+                            }
+                            __syncwarp();
+                            if (more) {
+                                if (x == 0 && !(ok = wait(sh.kv_full[stage], phase))) break;
+                                tc_fence_after();
+                                if (elect_one()) {
+                                    s_mma(x, x, stage);
+                                    if (x == 1) umma_commit(smem_u32(&sh.kv_empty[stage]));
+                                }
+                                __syncwarp();
+                            }
+                        }
+                        if (more) step();
+                    }
+                }
+                if (!ok) break;
+                if (elect_one()) {
+                    umma_commit(smem_u32(&sh.q_empty));
+                    umma_commit(smem_u32(&sh.o_full[0]));
+                    umma_commit(smem_u32(&sh.o_full[1]));
+                }
+                __syncwarp();
+            }
+            // the last MMAs are complete before shared and tensor memory are given back
+            if (elect_one()) umma_commit(smem_u32(&sh.drained));
+            __syncwarp();
+            mbar_wait_parity(smem_u32(&sh.drained), 0u);
+        } else {
+            // ------------------------------------------------ softmax
+            const int x = warp >> 2, row = tid & 127;
+            const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+            const uint32_t col_s = tmem + kC_ColS + x * 128 + lanes, col_o = tmem + kC_ColO + x * 128 + lanes;
+            const float scale = fabsf(a.scale_log2), sign = a.scale_log2 < 0.0f ? -1.0f : 1.0f;
+            uint32_t s_phase = 0, j_phase = 0;
+            // all softmax threads have come this far (bounded, as a barrier of the hardware would not be)
+            auto join = [&]() -> bool {
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&sh.joint));
+                const bool all = wait(sh.joint, j_phase);
+                j_phase ^= 1;
+                return all;
+            };
+            bool ok = true;
+            for (uint32_t part = 0; ok && walk.next(); ++part) {
+                const bool split = walk.unit.split;
+                const int n_rows = walk.unit.toks << a.log2g;
+                const int r = split ? row : x * 128 + row;               // row of the unit
+                const bool idle = ((split ? 0 : x * 128) + (warp & 3) * 32) >= n_rows;   // no row of this warp exists
+                const int rc = r < n_rows ? r : n_rows - 1;              // rows that do not exist follow the last that does
+                int limit = walk.s.n;                                    // tokens below it are seen
+                if (a.causal) {
+                    limit = walk.unit.first_pos + (rc >> a.log2g) + 1;
+                    if (limit < 0) limit = 0;
+                }
+                float m = -CUDART_INF_F, l = 0.0f;
+                bool any = false;                                        // O holds something
+                const int t0 = walk.t0, t1 = walk.t1;
+                for (int j = t0 + (split ? x : 0); j < t1; j += split ? 2 : 1) {
+                    if (!(ok = wait(sh.s_full[x], s_phase))) break;
+                    s_phase ^= 1;
+                    if (!idle) {
+                        tc_fence_after();
+                        const int seen = limit - j * kChunkTile;         // columns below it are seen
+                        const bool mask = __any_sync(0xffffffffu, seen < kChunkTile);
+                        float mx = -CUDART_INF_F;
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            uint32_t v[32];
+                            tmem_ld32(col_s + c * 32, v);
+                            tmem_wait_ld();
+                            if (mask) {
+#pragma unroll
+                                for (int i = 0; i < 32; ++i) mx = fmaxf(mx, c * 32 + i < seen ? sign * __uint_as_float(v[i]) : -CUDART_INF_F);
+                            } else {
+#pragma unroll
+                                for (int i = 0; i < 32; ++i) mx = fmaxf(mx, sign * __uint_as_float(v[i]));
+                            }
+                        }
+                        mx *= scale;
+                        if (!(mx > -CUDART_INF_F)) mx = -CUDART_INF_F;   // nothing seen, or 0 * inf
+                        const bool raise = mx > m + kC_Raise || (m == -CUDART_INF_F && mx > m);
+                        if (__any_sync(0xffffffffu, raise)) {
+                            const float m_new = raise ? mx : m;
+                            const float corr = raise ? exp2_approx(m - m_new) : 1.0f;
+                            l *= corr;
+                            m = m_new;
+                            if (any) {
+#pragma unroll
+                                for (int c = 0; c < 4; ++c) {
+                                    uint32_t v[32];
+                                    tmem_ld32(col_o + c * 32, v);
+                                    tmem_wait_ld();
+#pragma unroll
+                                    for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * corr);
+                                    tmem_st32(col_o + c * 32, v);
+                                }
+                            }
+                        }
+                        const float base = m == -CUDART_INF_F ? 0.0f : m, sc = sign * scale;
+                        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            uint32_t v[32], pk[16];
+                            tmem_ld32(col_s + c * 32, v);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) {
+                                float e = exp2_approx(fmaf(__uint_as_float(v[i]), sc, -base));
+                                if (mask && c * 32 + i >= seen) e = 0.0f;
+                                sum[i & 3] += e;
+                                v[i] = __float_as_uint(e);
+                            }
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) pk[i] = pack_bf16(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
+                            tmem_st16(col_s + c * 16, pk);
+                        }
+                        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                        any = true;
+                        tmem_wait_st();
+                        tc_fence_before();
+                    }
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(smem_u32(&sh.p_full[x]));
+                }
+                if (!ok || !(ok = wait(sh.o_full[x], part & 1u))) break;
+                tc_fence_after();
+
+                // ---- join the halves, write the result or this part
+                const bool joined = split && t1 - t0 > 1;                // both halves have taken tiles
+                float w_own = 1.0f, w_other = 0.0f;
+                if (split) {
+                    sh.ml[x][row][0] = m;
+                    sh.ml[x][row][1] = l;
+                    tc_fence_before();
+                    if (!(ok = join())) break;
+                    tc_fence_after();
+                    const float m0 = sh.ml[0][row][0], l0 = sh.ml[0][row][1];
+                    const float m1 = joined ? sh.ml[1][row][0] : -CUDART_INF_F, l1 = joined ? sh.ml[1][row][1] : 0.0f;
+                    m = fmaxf(m0, m1);
+                    const float b = m == -CUDART_INF_F ? 0.0f : m;
+                    w_own = exp2_approx(m0 - b);                         // of half 0
+                    w_other = exp2_approx(m1 - b);                       // of half 1
+                    l = l0 * w_own + (joined ? l1 * w_other : 0.0f);
+                }
+                // half x of a split unit writes columns 64 x .. 64 x + 63 of the joined row; a row tile of its own all 128
+                const int c_lo = split ? 2 * x : 0, c_hi = split ? 2 * x + 2 : 4;
+                const bool mine = r < n_rows;
+                const long long out_row = ((long long)(walk.s.row0 + walk.unit.tok0 + (r >> a.log2g)) * a.Hkv + walk.h << a.log2g) + (r & ((1 << a.log2g) - 1));
+                const int slot = (int)blockIdx.x * 2 + (walk.cut && blockIdx.x == walk.first_cta ? 1 : 0);
+                const float inv = l > 0.0f ? __frcp_rn(l) : l == 0.0f ? 0.0f : l;   // nothing seen: 0; NaN stays
+                if (!idle) {
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        if (c < c_lo || c >= c_hi) continue;
+                        uint32_t v[32];
+                        tmem_ld32(tmem + kC_ColO + lanes + (split ? 0 : x * 128) + c * 32, v);
+                        tmem_wait_ld();
+                        if (split) {
+                            if (joined) {
+                                uint32_t o[32];
+                                tmem_ld32(tmem + kC_ColO + lanes + 128 + c * 32, o);
+                                tmem_wait_ld();
+#pragma unroll
+                                for (int i = 0; i < 32; ++i)
+                                    v[i] = __float_as_uint(__uint_as_float(v[i]) * w_own + __uint_as_float(o[i]) * w_other);
+                            } else {
+#pragma unroll
+                                for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * w_own);
+                            }
+                        }
+                        if (!mine) continue;
+                        if (walk.cut) {
+                            float4 *dst = reinterpret_cast<float4 *>(a.part_acc + ((long long)slot * kChunkRows + r) * kD + c * 32);
+#pragma unroll
+                            for (int i = 0; i < 8; ++i)
+                                __stcg(dst + i, make_float4(__uint_as_float(v[4 * i]), __uint_as_float(v[4 * i + 1]), __uint_as_float(v[4 * i + 2]), __uint_as_float(v[4 * i + 3])));
+                        } else {
+                            uint4 *dst = reinterpret_cast<uint4 *>(a.out + out_row * kD + c * 32);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                uint32_t w[4];
+#pragma unroll
+                                for (int k = 0; k < 4; ++k)
+                                    w[k] = l == 0.0f ? 0u : pack_bf16(__uint_as_float(v[8 * i + 2 * k]) * inv, __uint_as_float(v[8 * i + 2 * k + 1]) * inv);
+                                dst[i] = make_uint4(w[0], w[1], w[2], w[3]);
+                            }
+                        }
+                    }
+                    if (mine && (!split || x == 0)) {
+                        if (walk.cut)
+                            __stcg(reinterpret_cast<float2 *>(a.part_ml + ((long long)slot * kChunkRows + r) * 2), make_float2(m, l));
+                        else if (a.lse)
+                            a.lse[out_row] = l == 0.0f ? -CUDART_INF_F : (m + log2f(l)) * kLn2;
+                    }
+                }
+                tc_fence_before();
+                if (walk.cut) {
+                    // ---- the last of the unit's parts joins them
+                    __threadfence();
+                    if (!(ok = join())) break;
+                    if (tid == 0) {
+                        const int seen = atomicAdd(a.tickets + walk.first_cta, 1);
+                        sh.last_part = seen == walk.n_parts - 1;
+                        if (sh.last_part) a.tickets[walk.first_cta] = 0;
+                        __threadfence();
+                    }
+                    if (!(ok = join())) break;
+                    if (sh.last_part) {
+                        // slot 1 of the first CTA, slot 0 of the others; a thread takes four columns of a row
+                        const long long s0 = (long long)walk.first_cta * 2 + 1, s1 = (long long)(walk.first_cta + 1) * 2;
+                        const int np = walk.n_parts;
+                        for (int e = tid; e < n_rows * 32; e += kC_Softmax) {
+                            const int er = e >> 5, ec = (e & 31) * 4;
+                            auto at = [&](int k) -> long long { return (k == 0 ? s0 : s1 + 2 * (k - 1)) * kChunkRows + er; };
+                            float mm = -CUDART_INF_F;
+                            for (int k = 0; k < np; ++k) mm = fmaxf(mm, __ldcg(a.part_ml + at(k) * 2));
+                            const float b = mm == -CUDART_INF_F ? 0.0f : mm;
+                            float ll = 0.0f;
+                            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+                            for (int k = 0; k < np; ++k) {
+                                const float2 ml = __ldcg(reinterpret_cast<const float2 *>(a.part_ml + at(k) * 2));
+                                const float4 v = __ldcg(reinterpret_cast<const float4 *>(a.part_acc + at(k) * kD + ec));
+                                const float w = exp2_approx(ml.x - b);
+                                ll = fmaf(ml.y, w, ll);
+                                acc.x = fmaf(v.x, w, acc.x); acc.y = fmaf(v.y, w, acc.y);
+                                acc.z = fmaf(v.z, w, acc.z); acc.w = fmaf(v.w, w, acc.w);
+                            }
+                            const float i = ll == 0.0f ? 0.0f : ll > 0.0f ? __frcp_rn(ll) : ll;
+                            const long long orow = ((long long)(walk.s.row0 + walk.unit.tok0 + (er >> a.log2g)) * a.Hkv + walk.h << a.log2g) + (er & ((1 << a.log2g) - 1));
+                            uint2 w = make_uint2(0u, 0u);
+                            if (ll != 0.0f) w = make_uint2(pack_bf16(acc.x * i, acc.y * i), pack_bf16(acc.z * i, acc.w * i));
+                            *reinterpret_cast<uint2 *>(a.out + orow * kD + ec) = w;
+                            if (ec == 0 && a.lse) a.lse[orow] = ll == 0.0f ? -CUDART_INF_F : (mm + log2f(ll)) * kLn2;
+                        }
+                    }
+                }
+                if (split) ok = join();   // both halves have read both O before the next unit's first MMA may write them
+            }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 0) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+    }
+}
+
+// ---- workspace: header, tickets, parts
+size_t chunk_workspace_bytes() {
+    return kHeaderBytes + kChunkMaxCtas * 4 + (size_t)2 * kChunkMaxCtas * kChunkRows * (2 + kD) * 4;
+}
+
+cudaError_t launch_chunk_attn(int B, int Hq, int Hkv, float sm_scale, TensorView q, const int32_t *offsets, int n_rows, TensorView K,
+                              TensorView V, int n_pages, const int32_t *table, long long bt_sb, int shift, const int32_t *seq_lens,
+                              bool causal, uint16_t *out, float *lse, void *workspace, cudaStream_t st) {
+    ChunkArgs a;
+    a.q = q.ptr; a.q_sn = q.sn; a.q_sh = q.sh;
+    a.offsets = offsets; a.seq_lens = seq_lens; a.table = table;
+    a.K = K; a.V = V; a.bt_sb = bt_sb;
+    a.n_rows = n_rows; a.n_pages = n_pages; a.shift = shift; a.B = B; a.Hkv = Hkv; a.causal = causal;
+    a.log2g = 0;
+    while ((Hkv << a.log2g) < Hq) ++a.log2g;
+    a.max_ctas = kChunkMaxCtas;
+    a.scale_log2 = sm_scale * kLog2e;
+    a.out = out; a.lse = lse;
+    char *ws = reinterpret_cast<char *>(workspace);
+    a.status = reinterpret_cast<uint32_t *>(ws);
+    a.tickets = reinterpret_cast<int32_t *>(ws + kHeaderBytes);
+    a.part_ml = reinterpret_cast<float *>(ws + kHeaderBytes + kChunkMaxCtas * 4);
+    a.part_acc = a.part_ml + (size_t)2 * kChunkMaxCtas * kChunkRows * 2;
+    cudaError_t e = cudaFuncSetAttribute(chunk_attn_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kC_Smem);
+    if (e != cudaSuccess) return e;
+    int grid = sm_count();
+    if (grid > kChunkMaxCtas) grid = kChunkMaxCtas;
+    e = launch_pdl(chunk_attn_kernel, dim3(grid), dim3(kC_Threads), kC_Smem, st, a);
+    if (e != cudaSuccess) return e;
+    count_launch();
+    return cudaGetLastError();
+}
+
+} // namespace ha

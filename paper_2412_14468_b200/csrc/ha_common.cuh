@@ -18,6 +18,7 @@ constexpr int kMaxAttnCtas = 1024;  // persistent CTAs of the attention kernel (
 constexpr int kMaxBalancedUnits = 1024;   // above this many (sequence, KV head) units: one CTA per unit
 constexpr int kMaxGroup = 8;        // query heads per KV head
 constexpr size_t kHeaderBytes = 256;   // device status word (+ padding)
+constexpr int kChunkMaxCtas = 160;       // CTAs of the attention of new tokens (bounds its tickets and parts)
 constexpr int kMaxUnits = 65536;       // (sequence, KV head) pairs: bounds the ticket region
 
 // Where each scratch region lives inside the caller's workspace.  All regions but the last depend
@@ -275,6 +276,12 @@ cudaError_t launch_gather_cluster(int B, int Hq, int Hkv, float sm_scale, const 
                                   const int32_t *count, int k_max, uint16_t *out, float *lse, uint32_t *status,
                                   cudaStream_t st, const int32_t *block_table = nullptr, long long bt_sb = 0,
                                   int page_shift = 0, int kv_shift = 0, bool in_step = false);   // kv_shift as in launch_attention
+
+// Attention of new tokens over a paged cache (ha_chunk.cu); the workspace has one size for all shapes.
+size_t chunk_workspace_bytes();
+cudaError_t launch_chunk_attn(int B, int Hq, int Hkv, float sm_scale, TensorView q, const int32_t *offsets, int n_rows, TensorView K,
+                              TensorView V, int n_pages, const int32_t *table, long long bt_sb, int shift, const int32_t *seq_lens,
+                              bool causal, uint16_t *out, float *lse, void *workspace, cudaStream_t st);
 
 // Signatures of 64 .. 512 bits through ENCODE and SCORE + TOPK (packed 64-bit words; strides in words).
 cudaError_t launch_encode_wide(const MapView &map, int n_bits, int heads_per_kv, TensorView x, int B, int H, int T,

@@ -13,6 +13,7 @@
 #include <Python.h>
 
 #include <ATen/core/TensorBase.h>
+#include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -381,6 +382,102 @@ HA_FN(gather_attn_paged) {
     });
 }
 
+// ---------------------------------------------------------------- new tokens over a paged cache
+
+// A tensor of the given type on the device that the call runs on.
+const at::Tensor &here(PyObject *o, at::ScalarType type, const char *name) {
+    const at::Tensor &t = tensor(o);
+    device_type(t, type, name);
+    if (t.get_device() != c10::cuda::current_device())
+        raise(PyExc_ValueError, std::string(name) + ": on another device than the current one");
+    return t;
+}
+template <typename T>
+T *dense(PyObject *o, at::ScalarType type, const char *name, int64_t least) {
+    const at::Tensor &t = here(o, type, name);
+    if (!t.is_contiguous() || t.numel() < least) raise(PyExc_ValueError, std::string(name) + ": expected a contiguous tensor of enough elements");
+    return reinterpret_cast<T *>(t.data_ptr());
+}
+template <typename T>
+T *dense_or_null(PyObject *o, at::ScalarType type, const char *name, int64_t least) {
+    return o == Py_None ? nullptr : dense<T>(o, type, name, least);
+}
+// bf16 [rows][heads][128] with a contiguous last dimension
+struct Packed {
+    ha_tensor t;
+    int32_t rows;
+};
+Packed packed(PyObject *o, const char *name, int32_t heads) {
+    const at::Tensor &t = here(o, at::kBFloat16, name);
+    if (t.dim() != 3 || t.size(2) != 128 || t.size(1) != heads || t.stride(2) != 1 || t.size(0) > INT32_MAX)
+        raise(PyExc_ValueError, std::string(name) + ": expected [rows, heads, 128] with a contiguous last dimension");
+    Packed p;
+    p.rows = (int32_t)t.size(0);
+    p.t.ptr = t.data_ptr();
+    p.t.stride_b = 0;
+    p.t.stride_h = t.size(1) > 1 ? t.stride(1) : 128;   // of a single head or row the stride is never used
+    p.t.stride_n = t.size(0) > 1 ? t.stride(0) : 128;
+    return p;
+}
+// bf16 [n_pages][Hkv][page_size][128]
+struct KvPool {
+    ha_tensor t;
+    int32_t pages;
+};
+KvPool kv_pool(PyObject *o, const char *name, int32_t heads, int32_t page_size) {
+    const at::Tensor &t = here(o, at::kBFloat16, name);
+    if (t.dim() != 4 || t.size(3) != 128 || t.stride(3) != 1 || t.size(1) != heads || t.size(2) != page_size || t.size(0) > INT32_MAX)
+        raise(PyExc_ValueError, std::string(name) + ": expected [pages, kv heads, page_size, 128] with a contiguous last dimension");
+    KvPool p;
+    p.pages = (int32_t)t.size(0);
+    p.t.ptr = t.data_ptr();
+    p.t.stride_b = t.stride(0);
+    p.t.stride_h = t.stride(1);
+    p.t.stride_n = t.size(2) > 1 ? t.stride(2) : 128;   // pages of one slot step through it in rows of 128
+    return p;
+}
+struct BlockTable {
+    const int32_t *p;
+    int64_t s0;
+    int32_t width;
+};
+BlockTable block_table(PyObject *o, int32_t sequences) {
+    const at::Tensor &t = here(o, at::kInt, "block_table");
+    if (t.dim() != 2 || t.size(0) < sequences || (t.size(1) > 1 && t.stride(1) != 1) || t.size(1) > INT32_MAX)
+        raise(PyExc_ValueError, "block_table: expected int32 [sequences, pages] with a contiguous last dimension");
+    return {reinterpret_cast<const int32_t *>(t.data_ptr()), t.stride(0), (int32_t)t.size(1)};
+}
+Workspace scratch(PyObject *o) {
+    if (o == Py_None) return {nullptr, 0};
+    const at::Tensor &t = tensor(o);
+    if (!t.is_cuda() || t.get_device() != c10::cuda::current_device() || !t.is_contiguous())
+        raise(PyExc_ValueError, "workspace: expected a contiguous tensor on the current device");
+    return {t.data_ptr(), (size_t)t.numel() * t.element_size()};
+}
+
+// shape, q, q_offsets, K_pool, V_pool, block_table, page_size, seq_lens, out, workspace, lse, causal, stream
+HA_FN(chunk_attn_paged) {
+    return guarded(n, 13, [&] {
+        const ha_shape *s = structure<ha_shape>(a[0]);
+        const int32_t ps = i32(a[6]);
+        const Packed q = packed(a[1], "q", s->n_q_heads);
+        const int32_t *off = dense<const int32_t>(a[2], at::kInt, "q_offsets", (int64_t)s->batch + 1);
+        const KvPool K = kv_pool(a[3], "K_pool", s->n_kv_heads, ps), V = kv_pool(a[4], "V_pool", s->n_kv_heads, ps);
+        const BlockTable bt = block_table(a[5], s->batch);
+        const int32_t *lens = dense<const int32_t>(a[7], at::kInt, "seq_lens", s->batch);
+        const int64_t rows_heads = (int64_t)q.rows * s->n_q_heads;
+        uint16_t *out = dense<uint16_t>(a[8], at::kBFloat16, "out", rows_heads * 128);
+        const Workspace w = scratch(a[9]);
+        float *lse = dense_or_null<float>(a[10], at::kFloat, "lse", rows_heads);
+        const int32_t causal = i32(a[11]);
+        if (K.pages != V.pages) raise(PyExc_ValueError, "K_pool and V_pool: different numbers of pages");
+        void *st = stream(a[12]);
+        return unlocked([&] {
+            return ha_chunk_attn_paged(s, &q.t, off, q.rows, &K.t, &V.t, K.pages, bt.p, bt.s0, ps, lens, causal, out, lse, w.p, w.n, st);
+        });
+    });
+}
+
 // shape, q, K, V, seq_lens, idx, count, k_max, out, lse, stream
 HA_FN(gather_attn_static) {
     return guarded(n, 11, [&] {
@@ -587,6 +684,7 @@ PyMethodDef kMethods[] = {
     HA_METHOD("gather_attn_per_head", gather_attn<&ha_gather_attn_per_head>),
     HA_METHOD("gather_attn_paged", gather_attn_paged<&ha_gather_attn_paged>),
     HA_METHOD("gather_attn_per_head_paged", gather_attn_paged<&ha_gather_attn_per_head_paged>),
+    HA_METHOD("chunk_attn_paged", chunk_attn_paged),
     HA_METHOD("gather_attn_static", gather_attn_static),
     HA_METHOD("dense_decode", dense_decode),
     HA_METHOD("sparse_decode", sparse_decode<&ha_sparse_decode>),
