@@ -62,6 +62,8 @@ extern "C" {
 #define HA_DEV_TIMEOUT 2u   /* a bounded wait inside a kernel gave up (ha_encode_prefill's tensor-core path,
                                ha_sparse_decode_pipelined, ha_chunk_attn_paged); the kernel returned early and its outputs are not valid */
 
+#define HA_DEV_NO_PAGE 4u   /* ha_pages_extend: not enough free pages, or a row of the block table is full; nothing was changed */
+
 #define HA_HEAD_DIM 128
 #define HA_N_BITS 32
 #define HA_HIST_BINS 33 /* scores 0..32 */
@@ -376,8 +378,9 @@ int ha_sparse_decode_paged_codes(const ha_shape *shape, const ha_mapping *map_q,
  *                may overlap other data, as in one projection output that holds q, k and v), multiples of 8
  *   q_offsets    i32 [batch + 1], ascending, within 0 .. n_rows (device); a sequence with bad ones is left out and raises
  *                HA_DEV_BAD_INDEX
- *   K_pool, V_pool, block_table, page_size   as in ha_gather_attn_paged; n_pages bounds the page numbers: tokens on a page outside
- *                0 .. n_pages - 1 read as zeros and raise HA_DEV_BAD_INDEX (the sequence's output is then of no use)
+ *   K_pool, V_pool, block_table, page_size   as in ha_gather_attn_paged, except that the two pools' strides need not agree; n_pages
+ *                bounds the page numbers: tokens on a page outside 0 .. n_pages - 1 read as zeros and raise HA_DEV_BAD_INDEX (the
+ *                sequence's output is then of no use)
  *   out          bf16 [n_rows][n_q_heads][128] contiguous; lse fp32 [n_rows][n_q_heads] or NULL
  *   workspace    ha_workspace_bytes_chunk() bytes, the same for all shapes; prepared once with ha_workspace_init
  * n_sink / n_local of the shape are not looked at.  Results do not depend on how the work is split: the same call gives the same
@@ -388,6 +391,93 @@ int ha_chunk_attn_paged(const ha_shape *shape, const ha_tensor *q, const int32_t
                         const ha_tensor *K_pool, const ha_tensor *V_pool, int32_t n_pages, const int32_t *block_table,
                         int64_t bt_stride_b, int32_t page_size, const int32_t *seq_lens, int32_t causal, uint16_t *out,
                         float *lse, void *workspace, size_t ws_bytes, void *stream);
+
+/* Rotary positions.  Pair i of the first rot_dim values of a head (values i and i + rot_dim / 2, or 2 i and 2 i + 1 if interleaved)
+ * at position p is turned by the angle p inv_freq[i]: (x, y) -> scale (x cos - y sin, x sin + y cos); the other values of the head
+ * pass through.  inverse != 0 turns by the negative angle (scale as it is): with the forward call's scale that is its gradient, with
+ * scale 1 / s it undoes a call of scale s, e.g. to move cached keys to other positions.  The angle is reduced to one turn in 64-bit
+ * integers, so far positions lose nothing; sines, cosines and products are fp32, one rounding to bf16.
+ *   x, y         bf16 rows [n_rows][n_heads][128]: stride_n steps over rows, stride_h over heads (stride_b is not used), multiples
+ *                of 8; y may be x (in place), else they must not overlap
+ *   inv_freq     f64 [rot_dim / 2], radians per position (device), e.g. from ha_rotary_freqs
+ *   rot_dim      multiple of 16, 16 .. 128
+ *   positions    i32 [n_rows] (device), any value */
+int ha_rotary(const ha_tensor *x, const ha_tensor *y, int32_t n_rows, int32_t n_heads, const double *inv_freq, int32_t rot_dim,
+              const int32_t *positions, int32_t interleaved, int32_t inverse, float scale, void *stream);
+
+/* The frequencies of the usual rules, on the HOST: inv_freq[i] = theta^(-2 i / rot_dim), changed for contexts `factor` times as
+ * long as the original_context that a model was trained on:
+ *   HA_ROTARY_PLAIN    as it is (factor and what follows are not used)
+ *   HA_ROTARY_LINEAR   all divided by factor (position interpolation)
+ *   HA_ROTARY_NTK      theta times factor^(rot_dim / (rot_dim - 2)): the slowest pair divided by factor, the fastest kept
+ *   HA_ROTARY_BANDS    pairs that turn fewer than `low` times over the original context are divided by factor, those of more than
+ *                      `high` turns kept, linear in the turns between (the rule of Llama 3.1: factor 8, low 1, high 4)
+ *   HA_ROTARY_YARN     the same idea by the pairs' numbers (arXiv 2309.00071): linear ramp between the pairs that turn `high` (32)
+ *                      and `low` (1) times, rounded outwards to whole pairs
+ * *scale (may be NULL) gets the factor for ha_rotary's scale: 0.1 ln(factor) + 1 for HA_ROTARY_YARN with factor > 1, else 1. */
+#define HA_ROTARY_PLAIN 0
+#define HA_ROTARY_LINEAR 1
+#define HA_ROTARY_NTK 2
+#define HA_ROTARY_BANDS 3
+#define HA_ROTARY_YARN 4
+int ha_rotary_freqs(int32_t rot_dim, double theta, int32_t rule, double factor, double low, double high, double original_context,
+                    double *inv_freq_host, float *scale);
+
+/* The new tokens' way into the paged cache in one launch: their queries turned into q_out, their keys turned and written to their
+ * pages, their values written to their pages.  Sequences, rows, pools and lengths as in ha_chunk_attn_paged (seq_lens count the new
+ * tokens already, their pages are allocated): row i of n new ones is token seq_lens[b] - n + i, at that position, or at
+ * positions[row] where positions is given.  A row whose token number is negative, or whose page lies outside 0 .. n_pages - 1
+ * (HA_DEV_BAD_INDEX), is turned but not written to the cache.  Two new tokens must not share a slot (ha_pages_extend sees to it).
+ *   q, k_new, v_new   bf16 rows [n_rows][heads][128] with strides as q of ha_chunk_attn_paged; q_out may be q
+ *   k_out             bf16 [n_rows][n_kv_heads][128] contiguous or NULL: the turned keys once more, packed (for ha_encode_append_paged,
+ *                     whose signatures belong to the keys as they are cached)
+ *   workspace         may be NULL; else one with the library's header: its status word takes HA_DEV_BAD_INDEX */
+int ha_rotary_append_paged(const ha_shape *shape, const ha_tensor *q, const ha_tensor *k_new, const ha_tensor *v_new,
+                           const ha_tensor *q_out, uint16_t *k_out, const int32_t *q_offsets, int32_t n_rows,
+                           const double *inv_freq, int32_t rot_dim, const int32_t *positions, int32_t interleaved, float scale,
+                           const ha_tensor *K_pool, const ha_tensor *V_pool, int32_t n_pages, const int32_t *block_table,
+                           int64_t bt_stride_b, int32_t page_size, const int32_t *seq_lens, void *workspace, void *stream);
+
+/* Pages: who holds which, and making room.  The state is three arrays of the caller's on the device, which these calls keep up:
+ *   seq_lens     i32 [batch] cached tokens of each sequence (0: the row is not in use)
+ *   block_table  i32 [batch][max_pages]: the first ceil(seq_len / page_size) entries of a row are its pages
+ *   ref_count    i32 [n_pages] how many rows hold a page; 0: free
+ * There is no other state: free pages are those of count 0, and are taken lowest number first, sequences and slots in ascending
+ * order, so the same state gives the same result.  workspace: ha_workspace_bytes_pages(n_pages, batch) bytes with the library's
+ * header (ha_workspace_init).  All calls can be captured.  page_size is a power of two.
+ *
+ *   ha_pages_fork     row children[i] becomes a copy of row parents[i] (i = 0 .. n_forks - 1): same length, same pages, each with
+ *                     one holder more.  Nothing is copied until ha_pages_extend writes into a shared page.  A fork whose child is in
+ *                     use (seq_len != 0), was listed before, or is a parent in the same call, or whose numbers lie outside the
+ *                     batch, is left out and raises HA_DEV_BAD_INDEX.  One parent may have many children.
+ *   ha_pages_extend   room for n_new[b] >= 0 tokens behind each sequence: new pages are entered in its row, and seq_lens[b] grows by
+ *                     n_new[b].  A sequence that grows and whose last page is partly filled and has other holders gets a page of its
+ *                     own in its place, with K, V and signatures copied (every holder that grows in the call does).  All or
+ *                     nothing: if the free pages do not suffice or a row would grow past max_pages, the call changes nothing and
+ *                     raises HA_DEV_NO_PAGE; negative numbers or pages outside the pool: nothing, HA_DEV_BAD_INDEX.
+ *   ha_pages_free     the listed rows end: each of their pages has one holder less, seq_len becomes 0; the entries of the row stay
+ *                     as they were.  A row listed again counts once.  A page that nobody holds raises HA_DEV_BAD_INDEX.
+ *   ha_pages_compact  all pages in use move to numbers below their count n_used: those at or above it move, in ascending order, into
+ *                     the free ones below it, in ascending order (K, V and signatures).  Writes block_table_out and ref_count_out
+ *                     (which may be block_table and ref_count themselves; entries behind a sequence's pages are copied),
+ *                     page_map[p] (where page p is now, -1 if it was free) and n_used.  The contents of pages that are free afterwards are left.
+ * code_pool may be NULL (a cache without signatures); strides as in ha_score_topk_paged. */
+size_t ha_workspace_bytes_pages(int32_t n_pages, int32_t batch);
+int ha_pages_fork(const int32_t *parents, const int32_t *children, int32_t n_forks, int32_t *seq_lens, int32_t batch,
+                  int32_t *block_table, int64_t bt_stride_b, int32_t max_pages, int32_t page_size, int32_t *ref_count,
+                  int32_t n_pages, void *workspace, size_t ws_bytes, void *stream);
+int ha_pages_extend(const int32_t *n_new, int32_t *seq_lens, int32_t batch, int32_t *block_table, int64_t bt_stride_b,
+                    int32_t max_pages, int32_t page_size, int32_t *ref_count, int32_t n_pages, int32_t n_kv_heads,
+                    const ha_tensor *K_pool, const ha_tensor *V_pool, uint32_t *code_pool, int64_t cp_stride_page,
+                    int64_t cp_stride_head, void *workspace, size_t ws_bytes, void *stream);
+int ha_pages_free(const int32_t *seqs, int32_t n_seqs, int32_t *seq_lens, int32_t batch, const int32_t *block_table,
+                  int64_t bt_stride_b, int32_t max_pages, int32_t page_size, int32_t *ref_count, int32_t n_pages, void *workspace,
+                  size_t ws_bytes, void *stream);
+int ha_pages_compact(const int32_t *seq_lens, int32_t batch, const int32_t *block_table, int64_t bt_stride_b, int32_t max_pages,
+                     int32_t page_size, const int32_t *ref_count, int32_t n_pages, int32_t n_kv_heads, const ha_tensor *K_pool,
+                     const ha_tensor *V_pool, uint32_t *code_pool, int64_t cp_stride_page, int64_t cp_stride_head,
+                     int32_t *block_table_out, int64_t bt_out_stride_b, int32_t *ref_count_out, int32_t *page_map, int32_t *n_used,
+                     void *workspace, size_t ws_bytes, void *stream);
 
 /* GATHER-ATT without a caller-provided workspace.  (The paper has no counterpart of this entry
  * point; it exists for integration reasons only.)

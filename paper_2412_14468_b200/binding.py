@@ -19,7 +19,8 @@ HOSTCALL_PATH = os.path.join(HERE, "_hostcall.so")
 
 HA_OK = 0
 HA_ERR_INVALID_ARG, HA_ERR_UNSUPPORTED, HA_ERR_WORKSPACE, HA_ERR_CUDA, HA_ERR_STATIC_LIMIT = 1, 2, 3, 4, 5
-HA_DEV_BAD_INDEX, HA_DEV_TIMEOUT = 1, 2
+HA_DEV_BAD_INDEX, HA_DEV_TIMEOUT, HA_DEV_NO_PAGE = 1, 2, 4
+HA_ROTARY_PLAIN, HA_ROTARY_LINEAR, HA_ROTARY_NTK, HA_ROTARY_BANDS, HA_ROTARY_YARN = range(5)
 HIST_BINS = 33
 
 EXPORTS = [
@@ -31,7 +32,8 @@ EXPORTS = [
     "ha_encode_wide", "ha_workspace_bytes_wide", "ha_score_topk_wide",
     "ha_score_topk_paged", "ha_score_topk_per_head_paged", "ha_gather_attn_per_head_paged", "ha_encode_append_paged",
     "ha_sparse_decode_paged_codes",
-    "ha_workspace_bytes_chunk", "ha_chunk_attn_paged",
+    "ha_workspace_bytes_chunk", "ha_chunk_attn_paged", "ha_rotary", "ha_rotary_freqs", "ha_rotary_append_paged",
+    "ha_workspace_bytes_pages", "ha_pages_fork", "ha_pages_extend", "ha_pages_free", "ha_pages_compact",
     "ha_kernel_launches", "ha_status_string", "ha_version",
 ]
 
@@ -111,7 +113,19 @@ def lib() -> C.CDLL:
         L.ha_score_topk_wide.restype = C.c_int
         L.ha_workspace_bytes_chunk.restype = SZ
         L.ha_chunk_attn_paged.argtypes = [P, P, P, I32, P, P, I32, P, I64, I32, P, I32, P, P, P, SZ, P]
-        L.ha_chunk_attn_paged.restype = C.c_int
+        F32, F64 = C.c_float, C.c_double
+        L.ha_rotary.argtypes = [P, P, I32, I32, P, I32, P, I32, I32, F32, P]
+        L.ha_rotary_freqs.argtypes = [I32, F64, I32, F64, F64, F64, F64, P, P]
+        L.ha_rotary_append_paged.argtypes = [P, P, P, P, P, P, P, I32, P, I32, P, I32, F32, P, P, I32, P, I64, I32, P, P, P]
+        L.ha_workspace_bytes_pages.restype = SZ
+        L.ha_workspace_bytes_pages.argtypes = [I32, I32]
+        L.ha_pages_fork.argtypes = [P, P, I32, P, I32, P, I64, I32, I32, P, I32, P, SZ, P]
+        L.ha_pages_extend.argtypes = [P, P, I32, P, I64, I32, I32, P, I32, I32, P, P, P, I64, I64, P, SZ, P]
+        L.ha_pages_free.argtypes = [P, I32, P, I32, P, I64, I32, I32, P, I32, P, SZ, P]
+        L.ha_pages_compact.argtypes = [P, I32, P, I64, I32, I32, P, I32, I32, P, P, P, I64, I64, P, I64, P, P, P, P, SZ, P]
+        for fn in ("ha_chunk_attn_paged", "ha_rotary", "ha_rotary_freqs", "ha_rotary_append_paged", "ha_pages_fork", "ha_pages_extend",
+                   "ha_pages_free", "ha_pages_compact"):
+            getattr(L, fn).restype = C.c_int
         L.ha_inner_products.argtypes = [P, P, I64, I64, P, P]
         L.ha_kernel_launches.restype = C.c_uint64
         L.ha_status_string.restype = C.c_char_p
@@ -401,6 +415,69 @@ def ha_chunk_attn_paged(shape: ha_shape, q, q_offsets, K_pool, V_pool, block_tab
     [rows, Hq, 128]; lse fp32 [rows, Hq]."""
     _check("ha_chunk_attn_paged", _host().chunk_attn_paged(shape, q, q_offsets, K_pool, V_pool, block_table, page_size, seq_lens, out,
                                                            workspace, lse, 1 if causal else 0, stream))
+
+
+def ha_rotary(x, out, inv_freq, positions, interleaved: bool = False, inverse: bool = False, scale: float = 1.0, stream=None) -> None:
+    """Rotary positions on x bf16 [rows, heads, 128] into out (may be x): inv_freq float64 [rot_dim / 2] radians per position,
+    positions int32 [rows].  inverse: turned back (the gradient of the forward call with the same scale)."""
+    _check("ha_rotary", _host().rotary(x, out, inv_freq, positions, 1 if interleaved else 0, 1 if inverse else 0, scale, stream))
+
+
+def ha_rotary_freqs(rot_dim: int, theta: float, rule: int = HA_ROTARY_PLAIN, factor: float = 1.0, low: float = 1.0, high: float = 4.0,
+                    original_context: float = 8192.0):
+    """(inv_freq float64 [rot_dim / 2] on the CPU, scale) by one of the HA_ROTARY_* rules."""
+    freq = torch.empty(max(0, rot_dim // 2), dtype=torch.float64)
+    scale = C.c_float(1.0)
+    _check("ha_rotary_freqs", lib().ha_rotary_freqs(rot_dim, theta, rule, factor, low, high, original_context, freq.data_ptr(), C.byref(scale)))
+    return freq, float(scale.value)
+
+
+def ha_rotary_append_paged(shape: ha_shape, q, k_new, v_new, q_out, inv_freq, q_offsets, K_pool, V_pool, block_table, page_size: int,
+                           seq_lens, workspace=None, k_out=None, positions=None, interleaved: bool = False, scale: float = 1.0,
+                           stream=None) -> None:
+    """New tokens into the paged cache: q bf16 [rows, Hq, 128] turned into q_out (may be q), k_new [rows, Hkv, 128] turned and written to
+    its pages (and to k_out), v_new written to its pages; rows packed by q_offsets, seq_lens count the new tokens already."""
+    _check("ha_rotary_append_paged", _host().rotary_append_paged(shape, q, k_new, v_new, q_out, inv_freq, q_offsets, K_pool, V_pool,
+                                                                 block_table, page_size, seq_lens, workspace, k_out, positions,
+                                                                 1 if interleaved else 0, scale, stream))
+
+
+def ha_workspace_bytes_pages(n_pages: int, batch: int) -> int:
+    n = int(lib().ha_workspace_bytes_pages(n_pages, batch))
+    if n == 0:
+        raise HashAttnError("ha_workspace_bytes_pages", HA_ERR_UNSUPPORTED)
+    return n
+
+
+def alloc_workspace_pages(n_pages: int, batch: int, device="cuda") -> torch.Tensor:
+    """A workspace for the ha_pages_* calls over so many pages and sequences, initialised."""
+    ws = torch.empty(ha_workspace_bytes_pages(n_pages, batch), dtype=torch.uint8, device=device)
+    ha_workspace_init(ws)
+    return ws
+
+
+def ha_pages_fork(parents, children, seq_lens, block_table, page_size: int, ref_count, workspace, stream=None) -> None:
+    """Rows children (int32 [n], not in use) of the block table become copies of rows parents; their pages get one holder more."""
+    _check("ha_pages_fork", _host().pages_fork(parents, children, seq_lens, block_table, page_size, ref_count, workspace, stream))
+
+
+def ha_pages_extend(n_new, seq_lens, block_table, page_size: int, ref_count, K_pool, V_pool, code_pool, workspace, stream=None) -> None:
+    """Room for n_new int32 [B] tokens behind each sequence, all or nothing (HA_DEV_NO_PAGE); a shared last page that is partly filled is
+    copied first.  code_pool int32 [n_pages, Hkv, page_size] or None."""
+    _check("ha_pages_extend", _host().pages_extend(n_new, seq_lens, block_table, page_size, ref_count, K_pool, V_pool, code_pool, workspace,
+                                                   stream))
+
+
+def ha_pages_free(seqs, seq_lens, block_table, page_size: int, ref_count, workspace, stream=None) -> None:
+    """The rows seqs (int32 [n]) end: their pages have one holder less, their length becomes 0."""
+    _check("ha_pages_free", _host().pages_free(seqs, seq_lens, block_table, page_size, ref_count, workspace, stream))
+
+
+def ha_pages_compact(seq_lens, block_table, page_size: int, ref_count, K_pool, V_pool, code_pool, block_table_out, ref_count_out, page_map,
+                     n_used, workspace, stream=None) -> None:
+    """All pages in use move below their number; block_table_out and ref_count_out may be block_table and ref_count themselves."""
+    _check("ha_pages_compact", _host().pages_compact(seq_lens, block_table, page_size, ref_count, K_pool, V_pool, code_pool, block_table_out,
+                                                     ref_count_out, page_map, n_used, workspace, stream))
 
 
 def ha_gather_attn_static(shape: ha_shape, q, K, V, seq_lens, idx, count, k_max: int, out, lse=None, stream=None) -> None:

@@ -1,6 +1,7 @@
 // C-ABI entry points: argument validation, workspace carving, kernel sequencing.
 // See include/hashattn.h for the contract of every function.
 #include <atomic>
+#include <cmath>
 
 #include "ha_common.cuh"
 
@@ -563,16 +564,13 @@ int ha_sparse_decode_paged_codes(const ha_shape *shape, const ha_mapping *map_q,
 
 // ---- new tokens over a paged cache
 
-// Pools of K and V rows in pages: a page is page_size consecutive slots, both pools step through pages in whole rows alike.
+// Pools of K and V rows in pages, each with strides of its own.
 static int check_paged_kv(const ha_tensor *K_pool, const ha_tensor *V_pool, int32_t n_pages, const int32_t *block_table,
                           int32_t page_size, int *shift) {
     HA_TRY(check_tensor(K_pool));
     HA_TRY(check_tensor(V_pool));
     if (!block_table || n_pages < 0) return HA_ERR_INVALID_ARG;
     if (page_size <= 0 || (page_size & (page_size - 1)) || page_size > 65536) return HA_ERR_INVALID_ARG;
-    if (K_pool->stride_b % K_pool->stride_n != 0 || V_pool->stride_b % V_pool->stride_n != 0 ||
-        K_pool->stride_b / K_pool->stride_n != V_pool->stride_b / V_pool->stride_n)
-        return HA_ERR_INVALID_ARG;
     *shift = 0;
     while ((1 << *shift) < page_size) ++*shift;
     return HA_OK;
@@ -600,6 +598,162 @@ int ha_chunk_attn_paged(const ha_shape *shape, const ha_tensor *q, const int32_t
     HA_CUDA(launch_chunk_attn(shape->batch, shape->n_q_heads, shape->n_kv_heads, shape->sm_scale, view(q), q_offsets, n_rows,
                               view(K_pool), view(V_pool), n_pages, block_table, bt_stride_b, shift, seq_lens, causal != 0, out, lse,
                               workspace, (cudaStream_t)stream));
+    return HA_OK;
+}
+
+static int check_turn(const double *inv_freq, int32_t rot_dim, float scale) {
+    if (!inv_freq || ((uintptr_t)inv_freq & 7) || !(scale == scale)) return HA_ERR_INVALID_ARG;
+    if (rot_dim < 16 || rot_dim > kD || (rot_dim & 15)) return HA_ERR_UNSUPPORTED;
+    return HA_OK;
+}
+
+int ha_rotary(const ha_tensor *x, const ha_tensor *y, int32_t n_rows, int32_t n_heads, const double *inv_freq, int32_t rot_dim,
+              const int32_t *positions, int32_t interleaved, int32_t inverse, float scale, void *stream) {
+    HA_TRY(check_rows(x));
+    HA_TRY(check_rows(y));
+    HA_TRY(check_turn(inv_freq, rot_dim, scale));
+    if (!positions || n_rows < 0 || n_heads <= 0) return HA_ERR_INVALID_ARG;
+    if (n_heads > 65535) return HA_ERR_UNSUPPORTED;
+    if (n_rows == 0) return HA_OK;
+    HA_CUDA(launch_rotary(view(x), view(y), n_rows, n_heads, inv_freq, rot_dim, positions, interleaved != 0, inverse != 0, scale,
+                          (cudaStream_t)stream));
+    return HA_OK;
+}
+
+int ha_rotary_freqs(int32_t rot_dim, double theta, int32_t rule, double factor, double low, double high, double original_context,
+                    double *inv_freq_host, float *scale) {
+    if (!inv_freq_host || !(theta > 1.0) || !std::isfinite(theta)) return HA_ERR_INVALID_ARG;
+    if (rot_dim < 16 || rot_dim > kD || (rot_dim & 15)) return HA_ERR_UNSUPPORTED;
+    if (rule < HA_ROTARY_PLAIN || rule > HA_ROTARY_YARN) return HA_ERR_INVALID_ARG;
+    if (rule != HA_ROTARY_PLAIN && (!(factor > 0.0) || !std::isfinite(factor))) return HA_ERR_INVALID_ARG;
+    const bool banded = rule == HA_ROTARY_BANDS || rule == HA_ROTARY_YARN;
+    if (banded && (!(low > 0.0) || !(high > low) || !(original_context > 0.0) || !std::isfinite(high) || !std::isfinite(original_context)))
+        return HA_ERR_INVALID_ARG;
+    const double kTwoPi = 6.283185307179586476925;
+    if (rule == HA_ROTARY_NTK) theta *= std::pow(factor, (double)rot_dim / (rot_dim - 2));
+    // the (fractional) pair that turns `turns` times over the original context
+    auto pair_of = [&](double turns) { return rot_dim * std::log(original_context / (turns * kTwoPi)) / (2.0 * std::log(theta)); };
+    double first = 0.0, last = 0.0;
+    if (rule == HA_ROTARY_YARN) {
+        first = std::floor(pair_of(high));
+        last = std::ceil(pair_of(low));
+        if (first < 0.0) first = 0.0;
+        if (last > rot_dim - 1) last = rot_dim - 1;
+        if (first == last) last += 1e-3;
+    }
+    for (int i = 0; i < rot_dim / 2; ++i) {
+        const double f = std::pow(theta, -2.0 * i / rot_dim);
+        double keep = 1.0;                                    // how much of the pair stays as it is
+        if (rule == HA_ROTARY_LINEAR) keep = 0.0;
+        else if (rule == HA_ROTARY_BANDS) keep = (original_context * f / kTwoPi - low) / (high - low);
+        else if (rule == HA_ROTARY_YARN) keep = 1.0 - (i - first) / (last - first);
+        keep = keep < 0.0 ? 0.0 : keep > 1.0 ? 1.0 : keep;
+        inv_freq_host[i] = rule == HA_ROTARY_PLAIN || rule == HA_ROTARY_NTK ? f : f * (keep + (1.0 - keep) / factor);
+    }
+    if (scale) *scale = rule == HA_ROTARY_YARN && factor > 1.0 ? (float)(0.1 * std::log(factor) + 1.0) : 1.0f;
+    return HA_OK;
+}
+
+int ha_rotary_append_paged(const ha_shape *shape, const ha_tensor *q, const ha_tensor *k_new, const ha_tensor *v_new,
+                           const ha_tensor *q_out, uint16_t *k_out, const int32_t *q_offsets, int32_t n_rows,
+                           const double *inv_freq, int32_t rot_dim, const int32_t *positions, int32_t interleaved, float scale,
+                           const ha_tensor *K_pool, const ha_tensor *V_pool, int32_t n_pages, const int32_t *block_table,
+                           int64_t bt_stride_b, int32_t page_size, const int32_t *seq_lens, void *workspace, void *stream) {
+    HA_TRY(check_shape(shape));
+    HA_TRY(check_rows(q));
+    HA_TRY(check_rows(k_new));
+    HA_TRY(check_rows(v_new));
+    HA_TRY(check_rows(q_out));
+    HA_TRY(check_turn(inv_freq, rot_dim, scale));
+    int shift;
+    HA_TRY(check_paged_kv(K_pool, V_pool, n_pages, block_table, page_size, &shift));
+    if (!q_offsets || !seq_lens || n_rows < 0 || ((uintptr_t)k_out & 15)) return HA_ERR_INVALID_ARG;
+    if (workspace && ((uintptr_t)workspace & 255)) return HA_ERR_WORKSPACE;
+    if (shape->batch == 0 || n_rows == 0) return HA_OK;
+    HA_CUDA(launch_rotary_append(shape->batch, shape->n_q_heads, shape->n_kv_heads, view(q), view(k_new), view(v_new), view(q_out), k_out,
+                                 q_offsets, n_rows, inv_freq, rot_dim, positions, interleaved != 0, scale, view(K_pool), view(V_pool),
+                                 n_pages, block_table, bt_stride_b, shift, seq_lens, reinterpret_cast<uint32_t *>(workspace),
+                                 (cudaStream_t)stream));
+    return HA_OK;
+}
+
+// ---- pages
+
+static int check_pages(const int32_t *seq_lens, int32_t batch, const int32_t *block_table, int64_t bt_stride_b, int32_t max_pages,
+                       int32_t page_size, const int32_t *ref_count, int32_t n_pages, const void *workspace, size_t ws_bytes, PagesView *v) {
+    if (!seq_lens || !block_table || !ref_count || batch < 0 || max_pages < 0 || n_pages < 0) return HA_ERR_INVALID_ARG;
+    if (page_size <= 0 || (page_size & (page_size - 1)) || page_size > 65536) return HA_ERR_INVALID_ARG;
+    if (batch > 1 && bt_stride_b < max_pages) return HA_ERR_INVALID_ARG;   // rows that are written must not overlap
+    if (batch > 65535) return HA_ERR_UNSUPPORTED;
+    if (!workspace || ((uintptr_t)workspace & 255) || ws_bytes < pages_workspace_bytes(n_pages, batch)) return HA_ERR_WORKSPACE;
+    int shift = 0;
+    while ((1 << shift) < page_size) ++shift;
+    *v = PagesView{const_cast<int32_t *>(seq_lens), const_cast<int32_t *>(block_table), const_cast<int32_t *>(ref_count),
+                   (long long)bt_stride_b, batch, max_pages, n_pages, shift};
+    return HA_OK;
+}
+static int check_page_pools(int32_t n_kv_heads, const ha_tensor *K_pool, const ha_tensor *V_pool) {
+    if (n_kv_heads <= 0) return HA_ERR_INVALID_ARG;
+    if (n_kv_heads > 65535) return HA_ERR_UNSUPPORTED;
+    HA_TRY(check_tensor(K_pool));
+    return check_tensor(V_pool);
+}
+
+size_t ha_workspace_bytes_pages(int32_t n_pages, int32_t batch) {
+    if (n_pages < 0 || batch < 0 || batch > 65535) return 0;
+    return pages_workspace_bytes(n_pages, batch);
+}
+
+int ha_pages_fork(const int32_t *parents, const int32_t *children, int32_t n_forks, int32_t *seq_lens, int32_t batch,
+                  int32_t *block_table, int64_t bt_stride_b, int32_t max_pages, int32_t page_size, int32_t *ref_count,
+                  int32_t n_pages, void *workspace, size_t ws_bytes, void *stream) {
+    PagesView v;
+    HA_TRY(check_pages(seq_lens, batch, block_table, bt_stride_b, max_pages, page_size, ref_count, n_pages, workspace, ws_bytes, &v));
+    if (n_forks < 0 || (n_forks > 0 && (!parents || !children))) return HA_ERR_INVALID_ARG;
+    if (n_forks > 65535) return HA_ERR_UNSUPPORTED;
+    if (n_forks == 0) return HA_OK;
+    HA_CUDA(launch_pages_fork(v, parents, children, n_forks, workspace, (cudaStream_t)stream));
+    return HA_OK;
+}
+
+int ha_pages_extend(const int32_t *n_new, int32_t *seq_lens, int32_t batch, int32_t *block_table, int64_t bt_stride_b,
+                    int32_t max_pages, int32_t page_size, int32_t *ref_count, int32_t n_pages, int32_t n_kv_heads,
+                    const ha_tensor *K_pool, const ha_tensor *V_pool, uint32_t *code_pool, int64_t cp_stride_page,
+                    int64_t cp_stride_head, void *workspace, size_t ws_bytes, void *stream) {
+    PagesView v;
+    HA_TRY(check_pages(seq_lens, batch, block_table, bt_stride_b, max_pages, page_size, ref_count, n_pages, workspace, ws_bytes, &v));
+    HA_TRY(check_page_pools(n_kv_heads, K_pool, V_pool));
+    if (!n_new || ((uintptr_t)code_pool & 3)) return HA_ERR_INVALID_ARG;
+    if (batch == 0) return HA_OK;
+    HA_CUDA(launch_pages_extend(v, n_new, view(K_pool), view(V_pool), n_kv_heads, code_pool, cp_stride_page, cp_stride_head, workspace,
+                                (cudaStream_t)stream));
+    return HA_OK;
+}
+
+int ha_pages_free(const int32_t *seqs, int32_t n_seqs, int32_t *seq_lens, int32_t batch, const int32_t *block_table,
+                  int64_t bt_stride_b, int32_t max_pages, int32_t page_size, int32_t *ref_count, int32_t n_pages, void *workspace,
+                  size_t ws_bytes, void *stream) {
+    PagesView v;
+    HA_TRY(check_pages(seq_lens, batch, block_table, bt_stride_b, max_pages, page_size, ref_count, n_pages, workspace, ws_bytes, &v));
+    if (n_seqs < 0 || (n_seqs > 0 && !seqs)) return HA_ERR_INVALID_ARG;
+    if (n_seqs > 65535) return HA_ERR_UNSUPPORTED;
+    if (n_seqs == 0) return HA_OK;
+    HA_CUDA(launch_pages_free(v, seqs, n_seqs, workspace, (cudaStream_t)stream));
+    return HA_OK;
+}
+
+int ha_pages_compact(const int32_t *seq_lens, int32_t batch, const int32_t *block_table, int64_t bt_stride_b, int32_t max_pages,
+                     int32_t page_size, const int32_t *ref_count, int32_t n_pages, int32_t n_kv_heads, const ha_tensor *K_pool,
+                     const ha_tensor *V_pool, uint32_t *code_pool, int64_t cp_stride_page, int64_t cp_stride_head,
+                     int32_t *block_table_out, int64_t bt_out_stride_b, int32_t *ref_count_out, int32_t *page_map, int32_t *n_used,
+                     void *workspace, size_t ws_bytes, void *stream) {
+    PagesView v;
+    HA_TRY(check_pages(seq_lens, batch, block_table, bt_stride_b, max_pages, page_size, ref_count, n_pages, workspace, ws_bytes, &v));
+    HA_TRY(check_page_pools(n_kv_heads, K_pool, V_pool));
+    if (!block_table_out || !ref_count_out || !page_map || !n_used || ((uintptr_t)code_pool & 3)) return HA_ERR_INVALID_ARG;
+    if (batch > 1 && bt_out_stride_b < max_pages) return HA_ERR_INVALID_ARG;
+    HA_CUDA(launch_pages_compact(v, view(K_pool), view(V_pool), n_kv_heads, code_pool, cp_stride_page, cp_stride_head, block_table_out,
+                                 bt_out_stride_b, ref_count_out, page_map, n_used, workspace, (cudaStream_t)stream));
     return HA_OK;
 }
 

@@ -283,6 +283,29 @@ cudaError_t launch_chunk_attn(int B, int Hq, int Hkv, float sm_scale, TensorView
                               TensorView V, int n_pages, const int32_t *table, long long bt_sb, int shift, const int32_t *seq_lens,
                               bool causal, uint16_t *out, float *lse, void *workspace, cudaStream_t st);
 
+// Rotary positions (ha_rotary.cu): x, y rows [rows][heads][128]; the append turns q and k and writes k and v into their pages.
+cudaError_t launch_rotary(TensorView x, TensorView y, int rows, int heads, const double *inv_freq, int rot_dim, const int32_t *positions,
+                          bool interleaved, bool inverse, float scale, cudaStream_t st);
+cudaError_t launch_rotary_append(int B, int Hq, int Hkv, TensorView q, TensorView k, TensorView v, TensorView q_out, uint16_t *k_out,
+                                 const int32_t *offsets, int rows, const double *inv_freq, int rot_dim, const int32_t *positions,
+                                 bool interleaved, float scale, TensorView K, TensorView V, int n_pages, const int32_t *table,
+                                 long long bt_sb, int shift, const int32_t *seq_lens, uint32_t *status, cudaStream_t st);
+
+// Pages of the cache (ha_pages.cu): block table [B][width], one count of holders per page.
+struct PagesView {
+    int32_t *seq_lens, *table, *ref;
+    long long bt_sb;
+    int B, width, n_pages, shift;
+};
+size_t pages_workspace_bytes(int n_pages, int B);
+cudaError_t launch_pages_fork(const PagesView &v, const int32_t *parents, const int32_t *children, int n, void *workspace, cudaStream_t st);
+cudaError_t launch_pages_free(const PagesView &v, const int32_t *seqs, int n, void *workspace, cudaStream_t st);
+cudaError_t launch_pages_extend(const PagesView &v, const int32_t *n_new, TensorView K, TensorView V, int heads, uint32_t *codes,
+                                long long c_page, long long c_head, void *workspace, cudaStream_t st);
+cudaError_t launch_pages_compact(const PagesView &v, TensorView K, TensorView V, int heads, uint32_t *codes, long long c_page,
+                                 long long c_head, int32_t *table_out, long long out_sb, int32_t *ref_out, int32_t *page_map,
+                                 int32_t *n_used, void *workspace, cudaStream_t st);
+
 // Signatures of 64 .. 512 bits through ENCODE and SCORE + TOPK (packed 64-bit words; strides in words).
 cudaError_t launch_encode_wide(const MapView &map, int n_bits, int heads_per_kv, TensorView x, int B, int H, int T,
                                uint64_t *codes, long long c_sb, long long c_sh, const int32_t *slot, cudaStream_t st);

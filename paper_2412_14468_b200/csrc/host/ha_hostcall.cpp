@@ -478,6 +478,176 @@ HA_FN(chunk_attn_paged) {
     });
 }
 
+// ---------------------------------------------------------------- rotary positions
+
+struct Freqs {
+    const double *p;
+    int32_t rot_dim;
+};
+Freqs freqs(PyObject *o) {
+    const double *p = dense<const double>(o, at::kDouble, "inv_freq", 1);
+    const int64_t half = tensor(o).numel();
+    return {p, half > 128 ? 256 : (int32_t)(2 * half)};
+}
+float f32(PyObject *o) {
+    const double v = PyFloat_AsDouble(o);
+    if (v == -1.0 && PyErr_Occurred()) throw Raised{};
+    return (float)v;
+}
+
+// x, out, inv_freq, positions, interleaved, inverse, scale, stream
+HA_FN(rotary) {
+    return guarded(n, 8, [&] {
+        const at::Tensor &xt = tensor(a[0]);
+        if (xt.dim() != 3) raise(PyExc_ValueError, "x: expected [rows, heads, 128] with a contiguous last dimension");
+        const int32_t heads = (int32_t)xt.size(1);
+        const Packed x = packed(a[0], "x", heads), y = packed(a[1], "out", heads);
+        if (x.rows != y.rows) raise(PyExc_ValueError, "x and out: different numbers of rows");
+        const Freqs f = freqs(a[2]);
+        const int32_t *pos = dense<const int32_t>(a[3], at::kInt, "positions", x.rows);
+        const int32_t interleaved = i32(a[4]), inverse = i32(a[5]);
+        const float scale = f32(a[6]);
+        void *st = stream(a[7]);
+        return unlocked([&] { return ha_rotary(&x.t, &y.t, x.rows, heads, f.p, f.rot_dim, pos, interleaved, inverse, scale, st); });
+    });
+}
+
+// shape, q, k_new, v_new, q_out, inv_freq, q_offsets, K_pool, V_pool, block_table, page_size, seq_lens, workspace, k_out, positions,
+// interleaved, scale, stream
+HA_FN(rotary_append_paged) {
+    return guarded(n, 18, [&] {
+        const ha_shape *s = structure<ha_shape>(a[0]);
+        const Packed q = packed(a[1], "q", s->n_q_heads), k = packed(a[2], "k_new", s->n_kv_heads), v = packed(a[3], "v_new", s->n_kv_heads),
+                     qo = packed(a[4], "q_out", s->n_q_heads);
+        if (k.rows != q.rows || v.rows != q.rows || qo.rows != q.rows) raise(PyExc_ValueError, "q, k_new, v_new, q_out: different numbers of rows");
+        const Freqs f = freqs(a[5]);
+        const int32_t *off = dense<const int32_t>(a[6], at::kInt, "q_offsets", (int64_t)s->batch + 1);
+        const int32_t ps = i32(a[10]);
+        const KvPool K = kv_pool(a[7], "K_pool", s->n_kv_heads, ps), V = kv_pool(a[8], "V_pool", s->n_kv_heads, ps);
+        if (K.pages != V.pages) raise(PyExc_ValueError, "K_pool and V_pool: different numbers of pages");
+        const BlockTable bt = block_table(a[9], s->batch);
+        const int32_t *lens = dense<const int32_t>(a[11], at::kInt, "seq_lens", s->batch);
+        const Workspace w = scratch(a[12]);
+        uint16_t *ko = dense_or_null<uint16_t>(a[13], at::kBFloat16, "k_out", (int64_t)q.rows * s->n_kv_heads * 128);
+        const int32_t *pos = dense_or_null<const int32_t>(a[14], at::kInt, "positions", q.rows);
+        const int32_t interleaved = i32(a[15]);
+        const float scale = f32(a[16]);
+        void *st = stream(a[17]);
+        return unlocked([&] {
+            return ha_rotary_append_paged(s, &q.t, &k.t, &v.t, &qo.t, ko, off, q.rows, f.p, f.rot_dim, pos, interleaved, scale, &K.t, &V.t,
+                                          K.pages, bt.p, bt.s0, ps, lens, w.p, st);
+        });
+    });
+}
+
+// ---------------------------------------------------------------- pages
+
+// The three arrays of the pages' state: seq_lens int32 [B], block_table int32 [B, pages], ref_count int32 [n_pages].
+struct Pages {
+    int32_t *lens, B;
+    int32_t *table;
+    int64_t s0;
+    int32_t width, size;
+    int32_t *ref, n_pages;
+    Pages(PyObject *seq_lens, PyObject *table_, PyObject *page_size, PyObject *ref_count) {
+        const at::Tensor &l = here(seq_lens, at::kInt, "seq_lens"), &r = here(ref_count, at::kInt, "ref_count");
+        if (l.numel() > INT32_MAX || r.numel() > INT32_MAX) raise(PyExc_ValueError, "seq_lens, ref_count: too many elements");
+        B = (int32_t)l.numel();
+        n_pages = (int32_t)r.numel();
+        lens = dense<int32_t>(seq_lens, at::kInt, "seq_lens", 0);
+        ref = dense<int32_t>(ref_count, at::kInt, "ref_count", 0);
+        const BlockTable t = block_table(table_, B);
+        table = const_cast<int32_t *>(t.p);
+        s0 = t.s0;
+        width = t.width;
+        size = i32(page_size);
+    }
+};
+struct PagePools {
+    KvPool K, V;
+    int32_t heads;
+    uint32_t *codes = nullptr;
+    int64_t c_page = 0, c_head = 0;
+    PagePools(PyObject *k, PyObject *v, PyObject *c, const Pages &p) {
+        const at::Tensor &kt = tensor(k);
+        if (kt.dim() != 4) raise(PyExc_ValueError, "K_pool: expected [pages, kv heads, page_size, 128] with a contiguous last dimension");
+        heads = (int32_t)kt.size(1);
+        K = kv_pool(k, "K_pool", heads, p.size);
+        V = kv_pool(v, "V_pool", heads, p.size);
+        if (K.pages < p.n_pages || V.pages < p.n_pages) raise(PyExc_ValueError, "K_pool, V_pool: fewer pages than ref_count");
+        if (c == Py_None) return;
+        const at::Tensor &t = here(c, at::kInt, "code_pool");
+        if (t.dim() != 3 || t.size(0) < p.n_pages || t.size(1) != heads || t.size(2) != p.size || (t.size(2) > 1 && t.stride(2) != 1))
+            raise(PyExc_ValueError, "code_pool: expected int32 [pages, kv heads, page_size]");
+        codes = reinterpret_cast<uint32_t *>(t.data_ptr());
+        c_page = t.stride(0);
+        c_head = t.stride(1);
+    }
+};
+int32_t count_of(PyObject *o, const char *name) {
+    const at::Tensor &t = here(o, at::kInt, name);
+    if (t.numel() > INT32_MAX) raise(PyExc_ValueError, std::string(name) + ": too many elements");
+    return (int32_t)t.numel();
+}
+
+// parents, children, seq_lens, block_table, page_size, ref_count, workspace, stream
+HA_FN(pages_fork) {
+    return guarded(n, 8, [&] {
+        const int32_t m = count_of(a[0], "parents");
+        if (count_of(a[1], "children") != m) raise(PyExc_ValueError, "parents and children: different lengths");
+        const int32_t *parents = dense<const int32_t>(a[0], at::kInt, "parents", 0), *children = dense<const int32_t>(a[1], at::kInt, "children", 0);
+        const Pages p(a[2], a[3], a[4], a[5]);
+        const Workspace w = scratch(a[6]);
+        void *st = stream(a[7]);
+        return unlocked([&] { return ha_pages_fork(parents, children, m, p.lens, p.B, p.table, p.s0, p.width, p.size, p.ref, p.n_pages, w.p, w.n, st); });
+    });
+}
+
+// n_new, seq_lens, block_table, page_size, ref_count, K_pool, V_pool, code_pool, workspace, stream
+HA_FN(pages_extend) {
+    return guarded(n, 10, [&] {
+        const Pages p(a[1], a[2], a[3], a[4]);
+        const int32_t *add = dense<const int32_t>(a[0], at::kInt, "n_new", p.B);
+        const PagePools pools(a[5], a[6], a[7], p);
+        const Workspace w = scratch(a[8]);
+        void *st = stream(a[9]);
+        return unlocked([&] {
+            return ha_pages_extend(add, p.lens, p.B, p.table, p.s0, p.width, p.size, p.ref, p.n_pages, pools.heads, &pools.K.t, &pools.V.t,
+                                   pools.codes, pools.c_page, pools.c_head, w.p, w.n, st);
+        });
+    });
+}
+
+// seqs, seq_lens, block_table, page_size, ref_count, workspace, stream
+HA_FN(pages_free) {
+    return guarded(n, 7, [&] {
+        const int32_t m = count_of(a[0], "seqs");
+        const int32_t *seqs = dense<const int32_t>(a[0], at::kInt, "seqs", 0);
+        const Pages p(a[1], a[2], a[3], a[4]);
+        const Workspace w = scratch(a[5]);
+        void *st = stream(a[6]);
+        return unlocked([&] { return ha_pages_free(seqs, m, p.lens, p.B, p.table, p.s0, p.width, p.size, p.ref, p.n_pages, w.p, w.n, st); });
+    });
+}
+
+// seq_lens, block_table, page_size, ref_count, K_pool, V_pool, code_pool, block_table_out, ref_count_out, page_map, n_used, workspace, stream
+HA_FN(pages_compact) {
+    return guarded(n, 13, [&] {
+        const Pages p(a[0], a[1], a[2], a[3]);
+        const PagePools pools(a[4], a[5], a[6], p);
+        const BlockTable out = block_table(a[7], p.B);
+        if (out.width != p.width) raise(PyExc_ValueError, "block_table_out: another width than block_table");
+        int32_t *ref_out = dense<int32_t>(a[8], at::kInt, "ref_count_out", p.n_pages), *map = dense<int32_t>(a[9], at::kInt, "page_map", p.n_pages);
+        int32_t *used = dense<int32_t>(a[10], at::kInt, "n_used", 1);
+        const Workspace w = scratch(a[11]);
+        void *st = stream(a[12]);
+        return unlocked([&] {
+            return ha_pages_compact(p.lens, p.B, p.table, p.s0, p.width, p.size, p.ref, p.n_pages, pools.heads, &pools.K.t, &pools.V.t, pools.codes,
+                                    pools.c_page, pools.c_head, const_cast<int32_t *>(out.p), out.s0, ref_out, map, used, w.p, w.n, st);
+        });
+    });
+}
+
 // shape, q, K, V, seq_lens, idx, count, k_max, out, lse, stream
 HA_FN(gather_attn_static) {
     return guarded(n, 11, [&] {
@@ -685,6 +855,12 @@ PyMethodDef kMethods[] = {
     HA_METHOD("gather_attn_paged", gather_attn_paged<&ha_gather_attn_paged>),
     HA_METHOD("gather_attn_per_head_paged", gather_attn_paged<&ha_gather_attn_per_head_paged>),
     HA_METHOD("chunk_attn_paged", chunk_attn_paged),
+    HA_METHOD("rotary", rotary),
+    HA_METHOD("rotary_append_paged", rotary_append_paged),
+    HA_METHOD("pages_fork", pages_fork),
+    HA_METHOD("pages_extend", pages_extend),
+    HA_METHOD("pages_free", pages_free),
+    HA_METHOD("pages_compact", pages_compact),
     HA_METHOD("gather_attn_static", gather_attn_static),
     HA_METHOD("dense_decode", dense_decode),
     HA_METHOD("sparse_decode", sparse_decode<&ha_sparse_decode>),
