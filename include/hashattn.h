@@ -372,8 +372,8 @@ int ha_sparse_decode_paged_codes(const ha_shape *shape, const ha_mapping *map_q,
  * seq_lens[b] tokens (causal == 0):
  *     out = sum_t softmax_t(sm_scale <q, k_t>) v_t,   lse = log sum_t exp(sm_scale <q, k_t>).
  * fp32 accumulation; softmax weights enter the product with V as bf16; one rounding of out to bf16.  A row that sees no token
- * (more new tokens than cached ones) gives out = 0, lse = -inf.  Rows of q and out outside the sequences' ranges are neither
- * read nor written.  Tokens at or beyond seq_lens[b], and what lies in unused slots of a page, do not matter, NaN or not.
+ * (more new tokens than cached ones) gives out = 0, lse = -inf.  Rows of q and out outside the sequences' ranges do not matter and
+ * are not written.  Tokens at or beyond seq_lens[b], and what lies in unused slots of a page, do not matter, NaN or not.
  *   q            bf16 rows [n_rows][n_q_heads][128]: stride_n steps over tokens, stride_h over heads (stride_b is not used; heads
  *                may overlap other data, as in one projection output that holds q, k and v), multiples of 8
  *   q_offsets    i32 [batch + 1], ascending, within 0 .. n_rows (device); a sequence with bad ones is left out and raises

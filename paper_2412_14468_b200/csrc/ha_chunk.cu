@@ -13,7 +13,12 @@
 // and S of both, 128 columns each; P (bf16) overwrites the first half of the S that it comes from.
 //   warps 0 - 3, 4 - 7   softmax of row tile 0 / 1: one thread per row
 //   warp 8               issues the MMAs: S = Q K^T (K-major operands), O += P V (P from tensor memory, V N-major)
-//   warps 9 - 11         copy Q, K and V rows into the 128-byte swizzle, through the block table
+//   warp 9               copies Q, K and V tiles by TMA into the 128-byte swizzle: a box is the rows of one page (or 128 of them),
+//                        64 columns wide; a lane looks up a page and issues its box.  Not loaded: pages behind the last token
+//   warps 10, 11         the last V tile of a sequence that ends inside it: rows behind the end are zeros, as 0 times what lies
+//                        there need not be 0
+// Pages of fewer than 8 tokens (an atom of the swizzle has 8 rows) and strides that no tensor map takes: warps 9 - 11 copy 16-byte
+// pieces instead.
 // While one row tile is in its softmax the tensor cores work for the other.  A unit of at most 128 rows (a decoding sequence) uses
 // the same two halves for alternate key tiles and joins them at its end.
 // A unit cut between CTAs: each part writes m, l and O to the workspace; the part that arrives last joins them all, in the order of
@@ -24,6 +29,9 @@
 #include "ha_chunk_plan.h"
 #include "ha_encode_dev.cuh"
 #include "ha_umma.cuh"
+
+#include <cstring>
+#include <cuda.h>   // CUtensorMap (types only; the encoder is fetched through the runtime)
 
 namespace ha {
 
@@ -56,7 +64,7 @@ struct ChunkArgs {
 };
 
 struct ChunkShared {
-    unsigned long long kv_full[kC_Stages], kv_empty[kC_Stages], q_full, q_empty, s_full[2], p_full[2], o_full[2], joint, drained;
+    unsigned long long kv_full[kC_Stages], kv_empty[kC_Stages], tail_go[kC_Stages], q_full, q_empty, s_full[2], p_full[2], o_full[2], joint, drained;
     long long start_rest, total;
     long long warp_sums[kC_Threads / 32];
     int start_b;
@@ -72,7 +80,20 @@ __device__ __forceinline__ float exp2_approx(float x) {
     return y;
 }
 
-__global__ void __launch_bounds__(kC_Threads, 1) chunk_attn_kernel(const ChunkArgs a) {
+// box of the pool seen as [page][head][2 halves][slot][64]
+__device__ __forceinline__ void tma_load_rows(uint32_t dst, const CUtensorMap *map, int slot, int half, int head, int page, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];"
+                 ::"r"(dst), "l"(map), "r"(0), "r"(slot), "r"(half), "r"(head), "r"(page), "r"(bar) : "memory");
+}
+// box of q seen as [2 halves][row][head][64]: 128 / G tokens of G heads, half after half
+__device__ __forceinline__ void tma_load_q(uint32_t dst, const CUtensorMap *map, int head, int row, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+                 ::"r"(dst), "l"(map), "r"(0), "r"(head), "r"(row), "r"(0), "r"(bar) : "memory");
+}
+
+template <bool kTma>
+__global__ void __launch_bounds__(kC_Threads, 1) chunk_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+                                                                  const __grid_constant__ CUtensorMap map_v, const ChunkArgs a) {
     extern __shared__ __align__(1024) unsigned char smem[];
     __shared__ __align__(8) ChunkShared sh;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -80,10 +101,11 @@ __global__ void __launch_bounds__(kC_Threads, 1) chunk_attn_kernel(const ChunkAr
 
     if (tid == 0) {
         for (int i = 0; i < kC_Stages; ++i) {
-            mbar_init(smem_u32(&sh.kv_full[i]), kC_Load);
+            mbar_init(smem_u32(&sh.kv_full[i]), kTma ? 2 : kC_Load);
             mbar_init(smem_u32(&sh.kv_empty[i]), 1);
+            mbar_init(smem_u32(&sh.tail_go[i]), 1);
         }
-        mbar_init(smem_u32(&sh.q_full), kC_Load);
+        mbar_init(smem_u32(&sh.q_full), kTma ? 1 : kC_Load);
         mbar_init(smem_u32(&sh.q_empty), 1);
         for (int x = 0; x < 2; ++x) {
             mbar_init(smem_u32(&sh.s_full[x]), 1);
@@ -176,8 +198,98 @@ __global__ void __launch_bounds__(kC_Threads, 1) chunk_attn_kernel(const ChunkAr
         walk.seq_lens = a.seq_lens; walk.offsets = a.offsets;
         walk.begin(blockIdx.x, sh.start_b, sh.start_rest);
 
-        if (warp > kC_Mma) {
-            // ------------------------------------------------ copies
+        if (kTma && warp == kC_Mma + 1) {
+            // ------------------------------------------------ copies by TMA
+            const int box = a.shift < 7 ? 1 << a.shift : kChunkTile, boxes = kChunkTile / box;   // rows of a box, boxes of a tile and half
+            const int half = lane / boxes, which = lane % boxes;
+            int stage = 0;
+            uint32_t phase = 1, issued = 0, issued_q = 0;   // phase of kv_empty: the ring starts empty
+            auto load = [&](const CUtensorMap *map, int j, bool left_out) -> bool {
+                const int tok = j * kChunkTile + which * box;
+                const bool mine = half < 2 && tok < walk.s.n && !left_out;
+                int page = 0;
+                if (mine) {
+                    page = __ldg(a.table + (long long)walk.b * a.bt_sb + (tok >> a.shift));
+                    if ((unsigned)page >= (unsigned)a.n_pages) {   // outside of the tensor map: zeros
+                        page = -1;
+                        if (a.status) atomicOr(a.status, HA_DEV_BAD_INDEX);
+                    }
+                }
+                if (!wait(sh.kv_empty[stage], phase)) return false;
+                if (!left_out) {
+                    const int there = (walk.s.n - j * kChunkTile + box - 1) / box;
+                    const uint32_t bar = smem_u32(&sh.kv_full[stage]);
+                    if (lane < 2) mbar_expect_tx(bar, (uint32_t)(there < boxes ? there : boxes) * box * 128);
+                    __syncwarp();
+                    if (mine)
+                        tma_load_rows(smem0 + kC_OffRing + stage * kC_TileBytes + half * kC_Half + which * box * 128, map,
+                                      tok & ((1 << a.shift) - 1), half, walk.h, page, bar);
+                } else if (lane == 0) {
+                    mbar_arrive(smem_u32(&sh.tail_go[stage]));   // the slot is empty: the tail's warps may fill it
+                }
+                __syncwarp();
+                ++issued;
+                if (++stage == kC_Stages) { stage = 0; phase ^= 1; }
+                return true;
+            };
+            bool ok = true;
+            for (uint32_t part = 0; ok && walk.next(); ++part) {
+                const int t0 = walk.t0, t1 = walk.t1;
+                const bool tail = (long long)t1 * kChunkTile > walk.s.n;
+                // the order in which the issuing warp waits for them; q behind the first keys, which need not wait for its place
+                const int lead = walk.unit.split ? 2 : 1;
+                for (int j = t0; ok && j < t0 + lead && j < t1; ++j) ok = load(&map_k, j, false);
+                if (!ok || !(ok = part == 0 || wait(sh.q_empty, (part - 1) & 1u))) break;
+                ++issued_q;
+                if (elect_one()) {
+                    const int tiles = walk.unit.split ? 1 : 2, tokens = kChunkTile >> a.log2g;
+                    mbar_expect_tx(smem_u32(&sh.q_full), tiles * kC_TileBytes);
+                    for (int x = 0; x < tiles; ++x)
+                        tma_load_q(smem0 + kC_OffQ + x * kC_TileBytes, &map_q, walk.h << a.log2g, walk.s.row0 + walk.unit.tok0 + x * tokens, smem_u32(&sh.q_full));
+                }
+                __syncwarp();
+                for (int j = t0; ok && j < t1; ++j) {
+                    ok = load(&map_v, j, tail && j == t1 - 1);
+                    if (ok && j + lead < t1) ok = load(&map_k, j + lead, false);
+                }
+            }
+            if (!ok) {   // never seen: what is in flight lands (one more bounded wait each) before shared memory is given up
+                for (uint32_t i = issued > kC_Stages ? issued - kC_Stages : 0; i < issued; ++i)
+                    mbar_wait_parity(smem_u32(&sh.kv_full[i % kC_Stages]), (i / kC_Stages) & 1u);
+                if (issued_q > 0) mbar_wait_parity(smem_u32(&sh.q_full), (issued_q - 1) & 1u);
+            }
+        } else if (kTma && warp > kC_Mma + 1) {
+            // ------------------------------------------------ the V tile that a sequence ends in, one half of its columns
+            const int half = warp - kC_Mma - 2, ch = lane & 7;
+            uint32_t stage_next = 0, phases = 0;      // slot of the part's first tile; of each slot, the phase of tail_go
+            while (walk.next()) {
+                stage_next = (stage_next + 2u * (uint32_t)(walk.t1 - walk.t0)) % kC_Stages;
+                if ((long long)walk.t1 * kChunkTile <= walk.s.n) continue;
+                const uint32_t stage = (stage_next + kC_Stages - 1) % kC_Stages;   // the part's last tile
+                // told by the warp that takes the slots in order: a wait for the slot to be empty could meet an older phase
+                if (!wait(sh.tail_go[stage], phases >> stage & 1u)) break;
+                phases ^= 1u << stage;
+                const uint32_t dst = smem0 + kC_OffRing + stage * kC_TileBytes + half * kC_Half;
+#pragma unroll 8
+                for (int r = lane >> 3; r < kChunkTile; r += 4) {
+                    const int tok = (walk.t1 - 1) * kChunkTile + r;
+                    const uint16_t *src = nullptr;
+                    if (tok < walk.s.n) {
+                        const int page = __ldg(a.table + (long long)walk.b * a.bt_sb + (tok >> a.shift));
+                        if ((unsigned)page < (unsigned)a.n_pages)
+                            src = a.V.ptr + (long long)page * a.V.sb + (long long)walk.h * a.V.sh + (long long)(tok & ((1 << a.shift) - 1)) * a.V.sn;
+                    }
+                    cp_async16(dst + r * 128 + ((ch ^ (r & 7)) << 4), reinterpret_cast<const unsigned char *>(src ? src : a.V.ptr) + half * 128 + ch * 16,
+                               src ? 16u : 0u);
+                }
+                cp_async_commit();
+                cp_async_wait<0>();
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&sh.kv_full[stage]));
+            }
+        } else if (!kTma && warp > kC_Mma) {
+            // ------------------------------------------------ copies by threads
             const int p = tid - kC_Softmax - 32, pw = p >> 5, hw = lane >> 4, ch = lane & 15;
             const uint32_t piece = (uint32_t)(ch >> 3) * kC_Half;
             int stage = 0, pending = 0, oldest = 0;   // copies of `pending` tiles are not announced yet, the first in ring slot `oldest`
@@ -592,6 +704,43 @@ size_t chunk_workspace_bytes() {
     return kHeaderBytes + kChunkMaxCtas * 4 + (size_t)2 * kChunkMaxCtas * kChunkRows * (2 + kD) * 4;
 }
 
+// Tensor maps (bf16, strides in elements): q [n_rows][Hq][128] and a pool [n_pages][Hkv][page][128], both with the 128 columns as two
+// halves of 64; false if the driver's encoder is missing or the strides do not fit a tensor map.
+typedef CUresult (*EncodeTiled)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
+                                const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+static EncodeTiled encode_tiled() {
+    static const EncodeTiled fn = [] {
+        void *p = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess && q == cudaDriverEntryPointSuccess)
+            return reinterpret_cast<EncodeTiled>(p);
+        cudaGetLastError();
+        return (EncodeTiled) nullptr;
+    }();
+    return fn;
+}
+static bool encode_map(CUtensorMap *tm, int rank, const void *base, const cuuint64_t *dims, const cuuint64_t *strides, const cuuint32_t *box) {
+    const cuuint32_t step[5] = {1u, 1u, 1u, 1u, 1u};
+    const EncodeTiled fn = encode_tiled();
+    if (!fn) return false;
+    for (int i = 0; i < rank; ++i)
+        if (dims[i] == 0 || dims[i] > (1ull << 32) || (i + 1 < rank && (strides[i] == 0 || (strides[i] & 15) || strides[i] >= (1ull << 40)))) return false;
+    return fn(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void *>(base), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+static bool q_map(CUtensorMap *tm, TensorView q, int rows, int Hq, int log2g) {
+    const cuuint64_t dims[4] = {64u, (cuuint64_t)Hq, (cuuint64_t)rows, 2u};
+    const cuuint64_t strides[3] = {(cuuint64_t)q.sh * 2, (cuuint64_t)q.sn * 2, 128u};
+    const cuuint32_t box[4] = {64u, 1u << log2g, (cuuint32_t)(kChunkTile >> log2g), 2u};
+    return encode_map(tm, 4, q.ptr, dims, strides, box);
+}
+static bool pool_map(CUtensorMap *tm, TensorView T, int n_pages, int Hkv, int shift) {
+    const cuuint64_t dims[5] = {64u, 1ull << shift, 2u, (cuuint64_t)Hkv, (cuuint64_t)n_pages};
+    const cuuint64_t strides[4] = {(cuuint64_t)T.sn * 2, 128u, (cuuint64_t)T.sh * 2, (cuuint64_t)T.sb * 2};
+    const cuuint32_t box[5] = {64u, shift < 7 ? 1u << shift : (cuuint32_t)kChunkTile, 1u, 1u, 1u};
+    return encode_map(tm, 5, T.ptr, dims, strides, box);
+}
+
 cudaError_t launch_chunk_attn(int B, int Hq, int Hkv, float sm_scale, TensorView q, const int32_t *offsets, int n_rows, TensorView K,
                               TensorView V, int n_pages, const int32_t *table, long long bt_sb, int shift, const int32_t *seq_lens,
                               bool causal, uint16_t *out, float *lse, void *workspace, cudaStream_t st) {
@@ -610,11 +759,16 @@ cudaError_t launch_chunk_attn(int B, int Hq, int Hkv, float sm_scale, TensorView
     a.tickets = reinterpret_cast<int32_t *>(ws + kHeaderBytes);
     a.part_ml = reinterpret_cast<float *>(ws + kHeaderBytes + kChunkMaxCtas * 4);
     a.part_acc = a.part_ml + (size_t)2 * kChunkMaxCtas * kChunkRows * 2;
-    cudaError_t e = cudaFuncSetAttribute(chunk_attn_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kC_Smem);
+    CUtensorMap mq, mk, mv;
+    memset(&mq, 0, sizeof(mq));
+    memset(&mk, 0, sizeof(mk));
+    memset(&mv, 0, sizeof(mv));
+    const bool tma = shift >= 3 && q_map(&mq, q, n_rows, Hq, a.log2g) && pool_map(&mk, K, n_pages, Hkv, shift) && pool_map(&mv, V, n_pages, Hkv, shift);
+    cudaError_t e = cudaFuncSetAttribute(tma ? chunk_attn_kernel<true> : chunk_attn_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kC_Smem);
     if (e != cudaSuccess) return e;
     int grid = sm_count();
     if (grid > kChunkMaxCtas) grid = kChunkMaxCtas;
-    e = launch_pdl(chunk_attn_kernel, dim3(grid), dim3(kC_Threads), kC_Smem, st, a);
+    e = launch_pdl(tma ? chunk_attn_kernel<true> : chunk_attn_kernel<false>, dim3(grid), dim3(kC_Threads), kC_Smem, st, mq, mk, mv, a);
     if (e != cudaSuccess) return e;
     count_launch();
     return cudaGetLastError();
