@@ -39,6 +39,9 @@ constexpr int kC_Softmax = 256;                    // threads of the softmax rol
 constexpr int kC_Mma = kC_Softmax / 32;            // the issuing warp
 constexpr int kC_Load = 96;                        // threads that copy (12 warps in all: 168 registers a thread)
 constexpr int kC_Threads = kC_Softmax + 32 + kC_Load;
+// registers of a thread: 168 at launch, moved to the softmax warps, which hold a row of 128 scores
+constexpr int kC_RegsSoftmax = 208, kC_RegsOther = 88;
+static_assert(kC_RegsSoftmax * kC_Softmax + kC_RegsOther * (32 + kC_Load) <= 168 * kC_Threads, "no more than the block was launched with");
 constexpr int kC_TileBytes = kChunkTile * kD * 2;  // 32768: two halves of 64 columns, each 128 rows of 128 bytes
 constexpr int kC_Half = kC_TileBytes / 2;
 constexpr int kC_Stages = 5;                       // ring of K and V tiles
@@ -78,6 +81,30 @@ __device__ __forceinline__ float exp2_approx(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
+}
+
+// two 32-bit operations in one instruction
+__device__ __forceinline__ void fma2(float &x, float &y, float m, float a) {   // (x, y) = (x, y) * m + a
+    asm("{\n\t.reg .b64 v, f, c;\n\tmov.b64 v, {%0, %1};\n\tmov.b64 f, {%2, %2};\n\tmov.b64 c, {%3, %3};\n\t"
+        "fma.rn.f32x2 v, v, f, c;\n\tmov.b64 {%0, %1}, v;\n\t}" : "+f"(x), "+f"(y) : "f"(m), "f"(a));
+}
+__device__ __forceinline__ void add2(float &x, float &y, float a, float b) {
+    asm("{\n\t.reg .b64 v, w;\n\tmov.b64 v, {%0, %1};\n\tmov.b64 w, {%2, %3};\n\tadd.rn.f32x2 v, v, w;\n\tmov.b64 {%0, %1}, v;\n\t}"
+        : "+f"(x), "+f"(y) : "f"(a), "f"(b));
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+// all 128 columns of S of this thread's row
+__device__ __forceinline__ void load_scores(uint32_t at, float (&v)[128]) {
+    uint32_t r[4][32];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) tmem_ld32(at + c * 32, r[c]);
+    tmem_wait_ld();
+#pragma unroll
+    for (int i = 0; i < 128; ++i) v[i] = __uint_as_float(r[i >> 5][i & 31]);
 }
 
 // box of the pool seen as [page][head][2 halves][slot][64]
@@ -192,6 +219,7 @@ __global__ void __launch_bounds__(kC_Threads, 1) chunk_attn_kernel(const __grid_
         return sh.fail == 0;
     };
 
+    if (warp >= kC_Mma) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kC_RegsOther));
     if (busy && sh.start_b >= 0) {
         ChunkWalk walk;
         walk.W = W; walk.C = C; walk.log2g = a.log2g; walk.B = a.B; walk.Hkv = a.Hkv; walk.n_rows = a.n_rows; walk.causal = a.causal != 0;
@@ -479,10 +507,11 @@ __global__ void __launch_bounds__(kC_Threads, 1) chunk_attn_kernel(const __grid_
             mbar_wait_parity(smem_u32(&sh.drained), 0u);
         } else {
             // ------------------------------------------------ softmax
+            asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kC_RegsSoftmax));
             const int x = warp >> 2, row = tid & 127;
             const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
             const uint32_t col_s = tmem + kC_ColS + x * 128 + lanes, col_o = tmem + kC_ColO + x * 128 + lanes;
-            const float scale = fabsf(a.scale_log2), sign = a.scale_log2 < 0.0f ? -1.0f : 1.0f;
+            const float scale = a.scale_log2 > 0.0f ? a.scale_log2 : 1.0f;   // others are multiplied in beforehand
             uint32_t s_phase = 0, j_phase = 0;
             // all softmax threads have come this far (bounded, as a barrier of the hardware would not be)
             auto join = [&]() -> bool {
@@ -514,22 +543,26 @@ __global__ void __launch_bounds__(kC_Threads, 1) chunk_attn_kernel(const __grid_
                         tc_fence_after();
                         const int seen = limit - j * kChunkTile;         // columns below it are seen
                         const bool mask = __any_sync(0xffffffffu, seen < kChunkTile);
-                        float mx = -CUDART_INF_F;
+                        float v[128];
+                        load_scores(col_s, v);
+                        if (!(a.scale_log2 > 0.0f)) {
 #pragma unroll
-                        for (int c = 0; c < 4; ++c) {
-                            uint32_t v[32];
-                            tmem_ld32(col_s + c * 32, v);
-                            tmem_wait_ld();
-                            if (mask) {
-#pragma unroll
-                                for (int i = 0; i < 32; ++i) mx = fmaxf(mx, c * 32 + i < seen ? sign * __uint_as_float(v[i]) : -CUDART_INF_F);
-                            } else {
-#pragma unroll
-                                for (int i = 0; i < 32; ++i) mx = fmaxf(mx, sign * __uint_as_float(v[i]));
-                            }
+                            for (int i = 0; i < 128; ++i) v[i] *= a.scale_log2;
                         }
-                        mx *= scale;
-                        if (!(mx > -CUDART_INF_F)) mx = -CUDART_INF_F;   // nothing seen, or 0 * inf
+                        if (mask) {
+#pragma unroll
+                            for (int i = 0; i < 128; ++i)
+                                if (i >= seen) v[i] = -CUDART_INF_F;
+                        }
+                        float x4[4] = {v[0], v[1], v[2], v[3]};
+#pragma unroll
+                        for (int i = 4; i + 8 <= 124; i += 8) {
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) x4[k] = max3(x4[k], v[i + k], v[i + 4 + k]);
+                        }
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) x4[k] = fmaxf(x4[k], v[124 + k]);
+                        const float mx = max3(x4[0], x4[1], fmaxf(x4[2], x4[3])) * scale;
                         const bool raise = mx > m + kC_Raise || (m == -CUDART_INF_F && mx > m);
                         if (__any_sync(0xffffffffu, raise)) {
                             const float m_new = raise ? mx : m;
@@ -537,36 +570,35 @@ __global__ void __launch_bounds__(kC_Threads, 1) chunk_attn_kernel(const __grid_
                             l *= corr;
                             m = m_new;
                             if (any) {
-#pragma unroll
-                                for (int c = 0; c < 4; ++c) {
-                                    uint32_t v[32];
-                                    tmem_ld32(col_o + c * 32, v);
+#pragma unroll 1
+                                for (int c = 0; c < 8; ++c) {
+                                    uint32_t o[16];
+                                    tmem_ld16(col_o + c * 16, o);
                                     tmem_wait_ld();
 #pragma unroll
-                                    for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * corr);
-                                    tmem_st32(col_o + c * 32, v);
+                                    for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * corr);
+                                    tmem_st16(col_o + c * 16, o);
                                 }
                             }
                         }
-                        const float base = m == -CUDART_INF_F ? 0.0f : m, sc = sign * scale;
-                        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+                        const float base = m == -CUDART_INF_F ? 0.0f : -m;
+                        float s0 = 0.0f, s1 = 0.0f, s2 = 0.0f, s3 = 0.0f;
 #pragma unroll
                         for (int c = 0; c < 4; ++c) {
-                            uint32_t v[32], pk[16];
-                            tmem_ld32(col_s + c * 32, v);
-                            tmem_wait_ld();
+                            uint32_t pk[16];
 #pragma unroll
-                            for (int i = 0; i < 32; ++i) {
-                                float e = exp2_approx(fmaf(__uint_as_float(v[i]), sc, -base));
-                                if (mask && c * 32 + i >= seen) e = 0.0f;
-                                sum[i & 3] += e;
-                                v[i] = __float_as_uint(e);
+                            for (int i = 0; i < 16; ++i) {
+                                float &e0 = v[c * 32 + 2 * i], &e1 = v[c * 32 + 2 * i + 1];
+                                fma2(e0, e1, scale, base);
+                                e0 = exp2_approx(e0);
+                                e1 = exp2_approx(e1);
+                                if (i & 1) add2(s2, s3, e0, e1);
+                                else add2(s0, s1, e0, e1);
+                                pk[i] = pack_bf16(e0, e1);
                             }
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) pk[i] = pack_bf16(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
                             tmem_st16(col_s + c * 16, pk);
                         }
-                        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                        l += (s0 + s1) + (s2 + s3);
                         any = true;
                         tmem_wait_st();
                         tc_fence_before();
