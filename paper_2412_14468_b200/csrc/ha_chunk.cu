@@ -9,18 +9,21 @@
 // operands have one type: half a step, 2^-9 relative, on each weight, of independent sign; l sums the unrounded p.
 //
 // Work: see ha_chunk_plan.h.  A CTA holds two tiles of 128 query rows (tokens x heads of a group, so that one fetch of K and V
-// serves the whole group) and streams key tiles of 128 tokens through a ring in shared memory.  Tensor memory: O of both row tiles
-// and S of both, 128 columns each; P (bf16) overwrites the first half of the S that it comes from.
-//   warps 0 - 3, 4 - 7   softmax of row tile 0 / 1: one thread per row
-//   warp 8               issues the MMAs: S = Q K^T (K-major operands), O += P V (P from tensor memory, V N-major)
-//   warp 9               copies Q, K and V tiles by TMA into the 128-byte swizzle: a box is the rows of one page (or 128 of them),
-//                        64 columns wide; a lane looks up a page and issues its box.  Not loaded: pages behind the last token
-//   warps 10, 11         the last V tile of a sequence that ends inside it: rows behind the end are zeros, as 0 times what lies
-//                        there need not be 0
-// Pages of fewer than 8 tokens (an atom of the swizzle has 8 rows) and strides that no tensor map takes: warps 9 - 11 copy 16-byte
-// pieces instead.
-// While one row tile is in its softmax the tensor cores work for the other.  A unit of at most 128 rows (a decoding sequence) uses
-// the same two halves for alternate key tiles and joins them at its end.
+// serves the whole group) and streams key tiles of 128 tokens through two rings in shared memory.
+//   warps 0 - 3, 4 - 7   softmax of row tile 0 / 1: one thread per row, its 128 scores in registers
+//   warp 8               issues S = Q K^T (both operands K-major, in shared memory)
+//   warp 11              issues O += P V (P from tensor memory, V N-major)
+//   warps 9, 10          fetch K and q / V, through the block table, into the 128-byte swizzle
+// Tensor memory: O of both row tiles, P (bf16) of both, and ONE S of 128 columns that the two take turns at: scores stay there
+// only until the softmax warps have them in registers, so the next S of a row tile is ready before its softmax is done with
+// the last one, and neither waits for the other.  (With an S of its own for each row tile, overwritten by P, a tile's two
+// products and its softmax formed one chain of 3700 cycles, 2048 of them with the tensor cores at work.)
+// A unit of at most 128 rows (a decoding sequence) uses the two halves for alternate key tiles and joins them at its end.
+// Fetching: by TMA, a box for the rows of one page (or 128 of them).  A box costs 45 ns and 1.3 ns a row however it is issued (measured), so pages of 16
+// take 1.0 us for a K tile in two boxes a page (one for either half of the columns, which a K-major operand of 128 rows needs)
+// and 0.85 us for a V tile in one.  By threads: the V tile that a sequence ends in, as rows behind the end have to be
+// zeros (0 times what lies there need not be 0); and everything where pages have fewer than 8 tokens (the swizzle repeats every
+// 8 rows) or no tensor map takes the strides.
 // A unit cut between CTAs: each part writes m, l and O to the workspace; the part that arrives last joins them all, in the order of
 // the keys, so that results do not depend on the order of arrival.
 // Every wait is bounded: a waiter that gives up raises HA_DEV_TIMEOUT, all roles stop, the MMAs in flight are waited for and the
@@ -36,20 +39,18 @@
 namespace ha {
 
 constexpr int kC_Softmax = 256;                    // threads of the softmax roles
-constexpr int kC_Mma = kC_Softmax / 32;            // the issuing warp
-constexpr int kC_Load = 96;                        // threads that copy (12 warps in all: 168 registers a thread)
-constexpr int kC_Threads = kC_Softmax + 32 + kC_Load;
-// registers of a thread: 168 at launch, moved to the softmax warps, which hold a row of 128 scores
+constexpr int kC_WarpS = 8, kC_WarpK = 9, kC_WarpV = 10, kC_WarpO = 11;
+constexpr int kC_Threads = 384;                    // 12 warps: 168 registers a thread
+// of these, moved to the softmax warps, which hold a row of 128 scores
 constexpr int kC_RegsSoftmax = 208, kC_RegsOther = 88;
-static_assert(kC_RegsSoftmax * kC_Softmax + kC_RegsOther * (32 + kC_Load) <= 168 * kC_Threads, "no more than the block was launched with");
+static_assert(kC_RegsSoftmax * kC_Softmax + kC_RegsOther * (kC_Threads - kC_Softmax) <= 168 * kC_Threads, "no more than the block was launched with");
 constexpr int kC_TileBytes = kChunkTile * kD * 2;  // 32768: two halves of 64 columns, each 128 rows of 128 bytes
 constexpr int kC_Half = kC_TileBytes / 2;
-constexpr int kC_Stages = 5;                       // ring of K and V tiles
-constexpr int kC_OffQ = 0, kC_OffRing = 2 * kC_TileBytes;
-constexpr int kC_Smem = kC_OffRing + kC_Stages * kC_TileBytes;   // 229376
-constexpr int kC_Ahead = 3;                        // tiles whose copies are in flight before the oldest is waited for
+constexpr int kC_SlotsK = 2, kC_SlotsV = 3;
+constexpr int kC_OffQ = 0, kC_OffK = 2 * kC_TileBytes, kC_OffV = kC_OffK + kC_SlotsK * kC_TileBytes;
+constexpr int kC_Smem = kC_OffV + kC_SlotsV * kC_TileBytes;   // 229376
 constexpr float kC_Raise = 8.0f;                   // how far (log2) a maximum may lie above the one that is referred to
-constexpr uint32_t kC_ColS = 256, kC_ColO = 0;     // tensor-memory columns: O0, O1, S0, S1
+constexpr uint32_t kC_ColO = 0, kC_ColS = 256, kC_ColP = 384;   // tensor-memory columns: O0, O1, S, P0, P1
 
 struct ChunkArgs {
     const uint16_t *q;
@@ -57,7 +58,7 @@ struct ChunkArgs {
     const int32_t *offsets, *seq_lens, *table;
     TensorView K, V;
     long long bt_sb;
-    int n_rows, n_pages, shift, B, Hkv, log2g, causal, max_ctas;
+    int n_rows, n_pages, shift, B, Hkv, log2g, causal, max_ctas, log2box;
     float scale_log2;
     uint16_t *out;
     float *lse;
@@ -67,7 +68,8 @@ struct ChunkArgs {
 };
 
 struct ChunkShared {
-    unsigned long long kv_full[kC_Stages], kv_empty[kC_Stages], tail_go[kC_Stages], q_full, q_empty, s_full[2], p_full[2], o_full[2], joint, drained;
+    unsigned long long k_full[kC_SlotsK], k_empty[kC_SlotsK], v_full[kC_SlotsV], v_empty[kC_SlotsV], q_full, q_empty;
+    unsigned long long s_full[2], s_free, p_full[2], o_done[2], joint, drained;
     long long start_rest, total;
     long long warp_sums[kC_Threads / 32];
     int start_b;
@@ -107,7 +109,7 @@ __device__ __forceinline__ void load_scores(uint32_t at, float (&v)[128]) {
     for (int i = 0; i < 128; ++i) v[i] = __uint_as_float(r[i >> 5][i & 31]);
 }
 
-// box of the pool seen as [page][head][2 halves][slot][64]
+// box of a pool seen as [page][head][2 halves][slot][64]
 __device__ __forceinline__ void tma_load_rows(uint32_t dst, const CUtensorMap *map, int slot, int half, int head, int page, uint32_t bar) {
     asm volatile("cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];"
                  ::"r"(dst), "l"(map), "r"(0), "r"(slot), "r"(half), "r"(head), "r"(page), "r"(bar) : "memory");
@@ -116,6 +118,168 @@ __device__ __forceinline__ void tma_load_rows(uint32_t dst, const CUtensorMap *m
 __device__ __forceinline__ void tma_load_q(uint32_t dst, const CUtensorMap *map, int head, int row, uint32_t bar) {
     asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
                  ::"r"(dst), "l"(map), "r"(0), "r"(head), "r"(row), "r"(0), "r"(bar) : "memory");
+}
+
+// The fetching warps: tiles of K (and q) or of V, in the order of the parts.  log2 of the rows of a box: the rows of a V tile lie box
+// by box, in either half of the columns; those of a K tile half by half.
+template <bool kTma, bool kV, typename Wait>
+__device__ __forceinline__ void chunk_fetch(const ChunkArgs &a, ChunkWalk &walk, const CUtensorMap *map, const CUtensorMap *map_q, ChunkShared &sh,
+                                            uint32_t smem0, int lane, Wait wait) {
+    constexpr int kSlots = kV ? kC_SlotsV : kC_SlotsK;
+    const TensorView &T = kV ? a.V : a.K;
+    unsigned long long *full = kV ? sh.v_full : sh.k_full, *empty = kV ? sh.v_empty : sh.k_empty;
+    const uint32_t ring = smem0 + (kV ? kC_OffV : kC_OffK);
+    const int lbox = kTma ? a.log2box : 7, lboxes = 7 - lbox;   // log2 of the rows of a box, of the boxes of a tile
+    const int mask = (1 << a.shift) - 1, hw = lane >> 4, ch = lane & 15;
+    int slot = 0, pending = -1;                       // pending: slot whose copies by threads are not announced yet
+    uint32_t phase = 1, issued = 0, issued_q = 0;     // phase of `empty`: the ring starts empty
+    bool ok = true;
+
+    auto announce = [&]() {
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&full[pending]));
+        pending = -1;
+    };
+    auto bad_page = [&](int page) -> bool {           // a page outside of the pool: zeros
+        if ((unsigned)page < (unsigned)a.n_pages) return false;
+        if (a.status) atomicOr(a.status, HA_DEV_BAD_INDEX);
+        return true;
+    };
+    // Page numbers for the boxes, 32 at a time, a lane each: those at work and those behind them, which are on their way
+    int ahead = 0, pages0 = -1, pages1 = -1;
+    auto fetch_pages = [&](int batch) {
+        const int e = batch * 32 + lane;
+        int page = -1;
+        if ((long long)e << a.shift < walk.s.n) {
+            page = __ldg(a.table + (long long)walk.b * a.bt_sb + e);
+            if (bad_page(page)) page = -1;
+        }
+        if (batch & 1) pages1 = page;
+        else pages0 = page;
+    };
+    // ... and for the rows that threads copy: rows lane, lane + 32, ...
+    int row_pages[4];
+    auto look_up = [&](int j) {
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int tok = j * kChunkTile + g * 32 + lane;
+            row_pages[g] = -1;
+            if (tok < walk.s.n) {
+                row_pages[g] = __ldg(a.table + (long long)walk.b * a.bt_sb + (tok >> a.shift));
+                if (bad_page(row_pages[g])) row_pages[g] = -1;
+            }
+        }
+    };
+    auto copy_rows = [&](int j, uint32_t dst) {       // a half-warp copies a row of 256 bytes; rows that are not there: zeros
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+#pragma unroll 4
+            for (int i = 0; i < 16; ++i) {
+                const int r = g * 32 + 2 * i + hw, page = __shfl_sync(0xffffffffu, row_pages[g], 2 * i + hw);
+                const uint16_t *src = T.ptr + ch * 8;
+                if (page >= 0) src += (long long)page * T.sb + (long long)walk.h * T.sh + (long long)((j * kChunkTile + r) & mask) * T.sn;
+                const uint32_t at = kV ? ((uint32_t)(r >> lbox) << lbox) * 256 + (uint32_t)(ch >> 3) * (128u << lbox) + (uint32_t)(r & ((1 << lbox) - 1)) * 128
+                                       : (uint32_t)(ch >> 3) * kC_Half + (uint32_t)r * 128;
+                cp_async16(dst + at + (((ch & 7) ^ (r & 7)) << 4), src, page >= 0 ? 16u : 0u);
+            }
+        }
+        cp_async_commit();
+    };
+    auto load = [&](int j, bool by_threads) -> bool {
+        if (by_threads) look_up(j);
+        else {
+            const int batch = (j * kChunkTile >> a.shift) >> 5;
+            if (batch == ahead) fetch_pages(++ahead);
+        }
+        if (!mbar_test(smem_u32(&empty[slot]), phase)) {
+            if (pending >= 0) {                       // what is waited for may wait for these
+                cp_async_wait<0>();
+                announce();
+            }
+            if (!wait(empty[slot], phase)) return false;
+        }
+        const uint32_t dst = ring + slot * kC_TileBytes, bar = smem_u32(&full[slot]);
+        if (by_threads) {
+            copy_rows(j, dst);
+            if (pending >= 0) {
+                cp_async_wait<1>();
+                announce();
+            }
+            pending = slot;
+        } else {
+            // a lane for each box; boxes behind the end of the sequence are left out (their keys are masked, whatever they are)
+            const int which = lane & ((1 << lboxes) - 1), half = lane >> lboxes, tok = j * kChunkTile + (which << lbox);
+            const int batch = (j * kChunkTile >> a.shift) >> 5;
+            const int page = __shfl_sync(0xffffffffu, batch & 1 ? pages1 : pages0, (tok >> a.shift) & 31);
+            const int left = walk.s.n - j * kChunkTile, there = left >= kChunkTile ? 1 << lboxes : (left + (1 << lbox) - 1) >> lbox;
+            if (lane == 0) mbar_expect_tx(bar, ((uint32_t)there << lbox) * 256);
+            __syncwarp();
+            if (which < there && half < (kV ? 1 : 2))
+                tma_load_rows(dst + ((uint32_t)which << lbox) * (kV ? 256 : 128) + (kV ? 0 : half * kC_Half), map, tok & mask, kV ? 0 : half, walk.h, page, bar);
+            ++issued;
+            if (pending >= 0) {
+                cp_async_wait<0>();
+                announce();
+            }
+        }
+        __syncwarp();
+        if (++slot == kSlots) { slot = 0; phase ^= 1; }
+        return true;
+    };
+    for (uint32_t part = 0; ok && walk.next(); ++part) {
+        const int t0 = walk.t0, t1 = walk.t1;
+        const bool tail = !kTma || (kV && (long long)t1 * kChunkTile > walk.s.n);
+        if (kTma) {
+            ahead = (t0 * kChunkTile >> a.shift) >> 5;
+            fetch_pages(ahead);
+        }
+        for (int j = t0; ok && j < t1; ++j) {
+            ok = load(j, !kTma || (tail && j == t1 - 1));
+            if (kV || !ok || j > t0) continue;
+            // q, behind the first keys, which need not wait for its place
+            if (pending >= 0) {
+                cp_async_wait<0>();
+                announce();
+            }
+            if (!(ok = part == 0 || wait(sh.q_empty, (part - 1) & 1u))) break;
+            const int n_rows = walk.unit.toks << a.log2g, rows = n_rows <= kChunkTile ? kChunkTile : kChunkRows;
+            if (kTma) {
+                if (elect_one()) {
+                    mbar_expect_tx(smem_u32(&sh.q_full), rows * 256);
+                    for (int x = 0; x < rows / kChunkTile; ++x)
+                        tma_load_q(smem0 + kC_OffQ + x * kC_TileBytes, map_q, walk.h << a.log2g,
+                                   walk.s.row0 + walk.unit.tok0 + x * (kChunkTile >> a.log2g), smem_u32(&sh.q_full));
+                }
+                ++issued_q;
+            } else {
+                const uint16_t *q = a.q + (long long)(walk.s.row0 + walk.unit.tok0) * a.q_sn + (long long)(walk.h << a.log2g) * a.q_sh + ch * 8;
+#pragma unroll 8
+                for (int r = hw; r < rows; r += 2) {
+                    const bool in = r < n_rows;
+                    const uint16_t *src = in ? q + (long long)(r >> a.log2g) * a.q_sn + (long long)(r & ((1 << a.log2g) - 1)) * a.q_sh : q;
+                    cp_async16(smem0 + kC_OffQ + (r >> 7) * kC_TileBytes + (uint32_t)(ch >> 3) * kC_Half + (r & 127) * 128 + (((ch & 7) ^ (r & 7)) << 4), src,
+                               in ? 16u : 0u);
+                }
+                cp_async_commit();
+                cp_async_wait<0>();
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&sh.q_full));
+            }
+            __syncwarp();
+        }
+    }
+    cp_async_wait<0>();
+    if (pending >= 0) announce();
+    if (!ok && kTma) {   // never seen: what is in flight lands (one more bounded wait each) before shared memory is given up
+        for (int i = 0; i < kSlots && i < (int)issued; ++i) {
+            slot = slot == 0 ? kSlots - 1 : slot - 1;
+            if (slot == kSlots - 1) phase ^= 1;
+            mbar_wait_parity(smem_u32(&full[slot]), phase ^ 1);
+        }
+        if (issued_q > 0) mbar_wait_parity(smem_u32(&sh.q_full), (issued_q - 1) & 1u);
+    }
 }
 
 template <bool kTma>
@@ -127,20 +291,24 @@ __global__ void __launch_bounds__(kC_Threads, 1) chunk_attn_kernel(const __grid_
     const uint32_t smem0 = smem_u32(smem);
 
     if (tid == 0) {
-        for (int i = 0; i < kC_Stages; ++i) {
-            mbar_init(smem_u32(&sh.kv_full[i]), kTma ? 2 : kC_Load);
-            mbar_init(smem_u32(&sh.kv_empty[i]), 1);
-            mbar_init(smem_u32(&sh.tail_go[i]), 1);
+        for (int i = 0; i < kC_SlotsK; ++i) {
+            mbar_init(smem_u32(&sh.k_full[i]), 1);
+            mbar_init(smem_u32(&sh.k_empty[i]), 1);
         }
-        mbar_init(smem_u32(&sh.q_full), kTma ? 1 : kC_Load);
+        for (int i = 0; i < kC_SlotsV; ++i) {
+            mbar_init(smem_u32(&sh.v_full[i]), 1);
+            mbar_init(smem_u32(&sh.v_empty[i]), 1);
+        }
+        mbar_init(smem_u32(&sh.q_full), 1);
         mbar_init(smem_u32(&sh.q_empty), 1);
+        mbar_init(smem_u32(&sh.s_free), 4);
         for (int x = 0; x < 2; ++x) {
             mbar_init(smem_u32(&sh.s_full[x]), 1);
             mbar_init(smem_u32(&sh.p_full[x]), 4);
-            mbar_init(smem_u32(&sh.o_full[x]), 1);
+            mbar_init(smem_u32(&sh.o_done[x]), 1);
         }
         mbar_init(smem_u32(&sh.joint), kC_Softmax / 32);
-        mbar_init(smem_u32(&sh.drained), 1);
+        mbar_init(smem_u32(&sh.drained), 2);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         sh.fail = 0;
         sh.start_b = -1;
@@ -219,289 +387,88 @@ __global__ void __launch_bounds__(kC_Threads, 1) chunk_attn_kernel(const __grid_
         return sh.fail == 0;
     };
 
-    if (warp >= kC_Mma) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kC_RegsOther));
+    if (warp >= kC_WarpS) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kC_RegsOther));
     if (busy && sh.start_b >= 0) {
         ChunkWalk walk;
         walk.W = W; walk.C = C; walk.log2g = a.log2g; walk.B = a.B; walk.Hkv = a.Hkv; walk.n_rows = a.n_rows; walk.causal = a.causal != 0;
         walk.seq_lens = a.seq_lens; walk.offsets = a.offsets;
         walk.begin(blockIdx.x, sh.start_b, sh.start_rest);
 
-        if (kTma && warp == kC_Mma + 1) {
-            // ------------------------------------------------ copies by TMA
-            const int box = a.shift < 7 ? 1 << a.shift : kChunkTile, boxes = kChunkTile / box;   // rows of a box, boxes of a tile and half
-            const int half = lane / boxes, which = lane % boxes;
-            int stage = 0;
-            uint32_t phase = 1, issued = 0, issued_q = 0;   // phase of kv_empty: the ring starts empty
-            auto load = [&](const CUtensorMap *map, int j, bool left_out) -> bool {
-                const int tok = j * kChunkTile + which * box;
-                const bool mine = half < 2 && tok < walk.s.n && !left_out;
-                int page = 0;
-                if (mine) {
-                    page = __ldg(a.table + (long long)walk.b * a.bt_sb + (tok >> a.shift));
-                    if ((unsigned)page >= (unsigned)a.n_pages) {   // outside of the tensor map: zeros
-                        page = -1;
-                        if (a.status) atomicOr(a.status, HA_DEV_BAD_INDEX);
-                    }
-                }
-                if (!wait(sh.kv_empty[stage], phase)) return false;
-                if (!left_out) {
-                    const int there = (walk.s.n - j * kChunkTile + box - 1) / box;
-                    const uint32_t bar = smem_u32(&sh.kv_full[stage]);
-                    if (lane < 2) mbar_expect_tx(bar, (uint32_t)(there < boxes ? there : boxes) * box * 128);
-                    __syncwarp();
-                    if (mine)
-                        tma_load_rows(smem0 + kC_OffRing + stage * kC_TileBytes + half * kC_Half + which * box * 128, map,
-                                      tok & ((1 << a.shift) - 1), half, walk.h, page, bar);
-                } else if (lane == 0) {
-                    mbar_arrive(smem_u32(&sh.tail_go[stage]));   // the slot is empty: the tail's warps may fill it
-                }
-                __syncwarp();
-                ++issued;
-                if (++stage == kC_Stages) { stage = 0; phase ^= 1; }
-                return true;
-            };
+        if (warp == kC_WarpK) {
+            chunk_fetch<kTma, false>(a, walk, &map_k, &map_q, sh, smem0, lane, wait);
+        } else if (warp == kC_WarpV) {
+            chunk_fetch<kTma, true>(a, walk, &map_v, &map_q, sh, smem0, lane, wait);
+        } else if (warp == kC_WarpS) {
+            // ------------------------------------------------ S = Q K^T.  Item i of a part is row tile i % 2 and key tile i / 2, or, of
+            // a unit of one row tile, key tile i
+            constexpr uint32_t kIdesc = umma_idesc(128, 128, false);
+            const uint32_t col_s = __shfl_sync(0xffffffffu, tmem, 0) + kC_ColS;
+            int slot = 0;
+            uint32_t phase = 0, before = 0;               // before: items so far
             bool ok = true;
             for (uint32_t part = 0; ok && walk.next(); ++part) {
-                const int t0 = walk.t0, t1 = walk.t1;
-                const bool tail = (long long)t1 * kChunkTile > walk.s.n;
-                // the order in which the issuing warp waits for them; q behind the first keys, which need not wait for its place
-                const int lead = walk.unit.split ? 2 : 1;
-                for (int j = t0; ok && j < t0 + lead && j < t1; ++j) ok = load(&map_k, j, false);
-                if (!ok || !(ok = part == 0 || wait(sh.q_empty, (part - 1) & 1u))) break;
-                ++issued_q;
-                if (elect_one()) {
-                    const int tiles = walk.unit.split ? 1 : 2, tokens = kChunkTile >> a.log2g;
-                    mbar_expect_tx(smem_u32(&sh.q_full), tiles * kC_TileBytes);
-                    for (int x = 0; x < tiles; ++x)
-                        tma_load_q(smem0 + kC_OffQ + x * kC_TileBytes, &map_q, walk.h << a.log2g, walk.s.row0 + walk.unit.tok0 + x * tokens, smem_u32(&sh.q_full));
-                }
-                __syncwarp();
-                for (int j = t0; ok && j < t1; ++j) {
-                    ok = load(&map_v, j, tail && j == t1 - 1);
-                    if (ok && j + lead < t1) ok = load(&map_k, j + lead, false);
-                }
-            }
-            if (!ok) {   // never seen: what is in flight lands (one more bounded wait each) before shared memory is given up
-                for (uint32_t i = issued > kC_Stages ? issued - kC_Stages : 0; i < issued; ++i)
-                    mbar_wait_parity(smem_u32(&sh.kv_full[i % kC_Stages]), (i / kC_Stages) & 1u);
-                if (issued_q > 0) mbar_wait_parity(smem_u32(&sh.q_full), (issued_q - 1) & 1u);
-            }
-        } else if (kTma && warp > kC_Mma + 1) {
-            // ------------------------------------------------ the V tile that a sequence ends in, one half of its columns
-            const int half = warp - kC_Mma - 2, ch = lane & 7;
-            uint32_t stage_next = 0, phases = 0;      // slot of the part's first tile; of each slot, the phase of tail_go
-            while (walk.next()) {
-                stage_next = (stage_next + 2u * (uint32_t)(walk.t1 - walk.t0)) % kC_Stages;
-                if ((long long)walk.t1 * kChunkTile <= walk.s.n) continue;
-                const uint32_t stage = (stage_next + kC_Stages - 1) % kC_Stages;   // the part's last tile
-                // told by the warp that takes the slots in order: a wait for the slot to be empty could meet an older phase
-                if (!wait(sh.tail_go[stage], phases >> stage & 1u)) break;
-                phases ^= 1u << stage;
-                const uint32_t dst = smem0 + kC_OffRing + stage * kC_TileBytes + half * kC_Half;
-#pragma unroll 8
-                for (int r = lane >> 3; r < kChunkTile; r += 4) {
-                    const int tok = (walk.t1 - 1) * kChunkTile + r;
-                    const uint16_t *src = nullptr;
-                    if (tok < walk.s.n) {
-                        const int page = __ldg(a.table + (long long)walk.b * a.bt_sb + (tok >> a.shift));
-                        if ((unsigned)page < (unsigned)a.n_pages)
-                            src = a.V.ptr + (long long)page * a.V.sb + (long long)walk.h * a.V.sh + (long long)(tok & ((1 << a.shift) - 1)) * a.V.sn;
-                    }
-                    cp_async16(dst + r * 128 + ((ch ^ (r & 7)) << 4), reinterpret_cast<const unsigned char *>(src ? src : a.V.ptr) + half * 128 + ch * 16,
-                               src ? 16u : 0u);
-                }
-                cp_async_commit();
-                cp_async_wait<0>();
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&sh.kv_full[stage]));
-            }
-        } else if (!kTma && warp > kC_Mma) {
-            // ------------------------------------------------ copies by threads
-            const int p = tid - kC_Softmax - 32, pw = p >> 5, hw = lane >> 4, ch = lane & 15;
-            const uint32_t piece = (uint32_t)(ch >> 3) * kC_Half;
-            int stage = 0, pending = 0, oldest = 0;   // copies of `pending` tiles are not announced yet, the first in ring slot `oldest`
-            uint32_t phase = 1;                       // of kv_empty: the ring starts empty
-            auto announce = [&]() {                   // the oldest tile has landed for this thread
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                mbar_arrive(smem_u32(&sh.kv_full[oldest]));
-                oldest = oldest + 1 == kC_Stages ? 0 : oldest + 1;
-                --pending;
-            };
-            auto flush = [&]() {
-                cp_async_wait<0>();
-                while (pending > 0) announce();
-            };
-            // rows of key tile j of the part, K or V: every warp looks up all 128 pages, half-warps copy rows
-            auto load = [&](const TensorView &T, int j) -> bool {
-                long long off[4];
-#pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const int tok = j * kChunkTile + g * 32 + lane;
-                    off[g] = -1;
-                    if (tok < walk.s.n) {
-                        const int page = __ldg(a.table + (long long)walk.b * a.bt_sb + (tok >> a.shift));
-                        if ((unsigned)page < (unsigned)a.n_pages)
-                            off[g] = (long long)page * T.sb + (long long)walk.h * T.sh + (long long)(tok & ((1 << a.shift) - 1)) * T.sn;
-                        else if (a.status) atomicOr(a.status, HA_DEV_BAD_INDEX);
-                    }
-                }
-                if (!mbar_test(smem_u32(&sh.kv_empty[stage]), phase)) {
-                    flush();   // what is waited for may wait for these tiles
-                    if (!wait(sh.kv_empty[stage], phase)) return false;
-                }
-                const uint32_t dst = smem0 + kC_OffRing + stage * kC_TileBytes + piece;
-#pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    for (int i = (pw + 3 - (g * 16) % 3) % 3; i < 16; i += 3) {
-                        const int lr = 2 * i + hw, r = g * 32 + lr;
-                        const long long o = __shfl_sync(0xffffffffu, off[g], lr);
-                        cp_async16(dst + r * 128 + (((ch & 7) ^ (r & 7)) << 4),
-                                   reinterpret_cast<const unsigned char *>(T.ptr + (o >= 0 ? o : 0)) + ch * 16, o >= 0 ? 16u : 0u);
-                    }
-                }
-                cp_async_commit();
-                if (++stage == kC_Stages) { stage = 0; phase ^= 1; }
-                if (++pending > kC_Ahead) {
-                    cp_async_wait<kC_Ahead>();
-                    announce();
-                }
-                return true;
-            };
-            bool ok = true;
-            for (uint32_t part = 0; ok && walk.next(); ++part) {
-                flush();
-                if (part > 0 && !wait(sh.q_empty, (part - 1) & 1u)) break;
-                const int n_rows = walk.unit.toks << a.log2g;
-                const int rows = n_rows <= 128 ? 128 : 256;
-                const uint16_t *q = a.q + (long long)(walk.s.row0 + walk.unit.tok0) * a.q_sn + (long long)(walk.h << a.log2g) * a.q_sh;
-                for (int r = pw * 2 + hw; r < rows; r += kC_Load / 16) {
-                    const bool in = r < n_rows;
-                    const uint16_t *src = in ? q + (long long)(r >> a.log2g) * a.q_sn + (long long)(r & ((1 << a.log2g) - 1)) * a.q_sh : q;
-                    cp_async16(smem0 + kC_OffQ + (r >> 7) * kC_TileBytes + piece + (r & 127) * 128 + (((ch & 7) ^ (r & 7)) << 4),
-                               reinterpret_cast<const unsigned char *>(src) + ch * 16, in ? 16u : 0u);
-                }
-                cp_async_commit();
-                cp_async_wait<0>();
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                mbar_arrive(smem_u32(&sh.q_full));
-                const int t0 = walk.t0, t1 = walk.t1;
-                // the order in which the issuing warp waits for them
-                const int lead = walk.unit.split ? 2 : 1;
-                for (int j = t0; ok && j < t0 + lead && j < t1; ++j) ok = load(a.K, j);
-                for (int j = t0; ok && j < t1; ++j) {
-                    ok = load(a.V, j);
-                    if (ok && j + lead < t1) ok = load(a.K, j + lead);
-                }
-            }
-            flush();
-        } else if (warp == kC_Mma) {
-            // ------------------------------------------------ MMAs
-            constexpr uint32_t kIdescS = umma_idesc(128, 128, false), kIdescO = umma_idesc(128, 128, true);
-            const uint32_t base = __shfl_sync(0xffffffffu, tmem, 0);
-            int stage = 0;
-            uint32_t phase = 0, p_phase[2] = {0, 0};
-            auto step = [&]() { if (++stage == kC_Stages) { stage = 0; phase ^= 1; } };
-            auto s_mma = [&](int qx, int x, int at) {   // S_x = Q_qx K^T
-                const uint64_t qd = umma_desc_sw128(smem0 + kC_OffQ + qx * kC_TileBytes, 16, 1024);
-                const uint64_t kd = umma_desc_sw128(smem0 + kC_OffRing + at * kC_TileBytes, 16, 1024);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const uint64_t d = (uint64_t)((i >> 2) * (kC_Half >> 4) + (i & 3) * 2);
-                    umma_ss(base + kC_ColS + x * 128, qd + d, kd + d, kIdescS, i ? 1u : 0u);
-                }
-                umma_commit(smem_u32(&sh.s_full[x]));
-            };
-            auto o_mma = [&](int x, int at, bool add) {   // O_x += P_x V
-                const uint64_t vd = umma_desc_sw128(smem0 + kC_OffRing + at * kC_TileBytes, kC_Half, 1024);
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    umma_ts(base + kC_ColO + x * 128, base + kC_ColS + x * 128 + i * 8, vd + (uint64_t)(i * (2048 >> 4)), kIdescO, (add || i) ? 1u : 0u);
-            };
-            bool ok = true;
-            for (uint32_t part = 0; ok && walk.next(); ++part) {
-                const int n = walk.t1 - walk.t0;
+                const bool split = walk.unit.split;
+                const int n = (walk.t1 - walk.t0) * (split ? 1 : 2);
                 if (!(ok = wait(sh.q_full, part & 1u))) break;
-                if (walk.unit.split) {
-                    for (int j = 0; ok && j < 2 && j < n; ++j) {
-                        if (!(ok = wait(sh.kv_full[stage], phase))) break;
-                        tc_fence_after();
-                        if (elect_one()) {
-                            s_mma(0, j, stage);
-                            umma_commit(smem_u32(&sh.kv_empty[stage]));
-                        }
-                        __syncwarp();
-                        step();
-                    }
-                    for (int j = 0; ok && j < n; ++j) {
-                        const int x = j & 1;
-                        ok = wait(sh.kv_full[stage], phase) && wait(sh.p_full[x], p_phase[x]);
-                        if (!ok) break;
-                        p_phase[x] ^= 1;
-                        tc_fence_after();
-                        if (elect_one()) {
-                            o_mma(x, stage, j >= 2);
-                            umma_commit(smem_u32(&sh.kv_empty[stage]));
-                        }
-                        __syncwarp();
-                        step();
-                        if (j + 2 < n) {
-                            if (!(ok = wait(sh.kv_full[stage], phase))) break;
-                            tc_fence_after();
-                            if (elect_one()) {
-                                s_mma(0, x, stage);
-                                umma_commit(smem_u32(&sh.kv_empty[stage]));
-                            }
-                            __syncwarp();
-                            step();
-                        }
-                    }
-                } else {
-                    if (!(ok = wait(sh.kv_full[stage], phase))) break;
+                for (int i = 0; i < n; ++i, ++before) {
+                    const int x = i & 1;
+                    if ((split || x == 0) && !(ok = wait(sh.k_full[slot], phase))) break;
+                    if (before > 0 && !(ok = wait(sh.s_free, (before - 1) & 1u))) break;
                     tc_fence_after();
                     if (elect_one()) {
-                        s_mma(0, 0, stage);
-                        s_mma(1, 1, stage);
-                        umma_commit(smem_u32(&sh.kv_empty[stage]));
+                        const uint64_t qd = umma_desc_sw128(smem0 + kC_OffQ + (split ? 0 : x) * kC_TileBytes, 16, 1024);
+                        const uint64_t kd = umma_desc_sw128(smem0 + kC_OffK + slot * kC_TileBytes, 16, 1024);
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) {
+                            const uint64_t d = (uint64_t)((k >> 2) * (kC_Half >> 4) + (k & 3) * 2);
+                            umma_ss(col_s, qd + d, kd + d, kIdesc, k ? 1u : 0u);
+                        }
+                        umma_commit(smem_u32(&sh.s_full[x]));
+                        if (split || x == 1) umma_commit(smem_u32(&sh.k_empty[slot]));
+                        if (i == n - 1) umma_commit(smem_u32(&sh.q_empty));
                     }
                     __syncwarp();
-                    step();
-                    for (int j = 0; ok && j < n; ++j) {
-                        const int v = stage;
-                        ok = wait(sh.kv_full[v], phase);
-                        step();
-                        const bool more = j + 1 < n;
-                        for (int x = 0; ok && x < 2; ++x) {
-                            if (!(ok = wait(sh.p_full[x], p_phase[x]))) break;
-                            p_phase[x] ^= 1;
-                            tc_fence_after();
-                            if (elect_one()) {
-                                o_mma(x, v, j > 0);
-                                if (x == 1) umma_commit(smem_u32(&sh.kv_empty[v]));
-                            }
-                            __syncwarp();
-                            if (more) {
-                                if (x == 0 && !(ok = wait(sh.kv_full[stage], phase))) break;
-                                tc_fence_after();
-                                if (elect_one()) {
-                                    s_mma(x, x, stage);
-                                    if (x == 1) umma_commit(smem_u32(&sh.kv_empty[stage]));
-                                }
-                                __syncwarp();
-                            }
-                        }
-                        if (more) step();
-                    }
+                    if ((split || x == 1) && ++slot == kC_SlotsK) { slot = 0; phase ^= 1; }
                 }
-                if (!ok) break;
-                if (elect_one()) {
-                    umma_commit(smem_u32(&sh.q_empty));
-                    umma_commit(smem_u32(&sh.o_full[0]));
-                    umma_commit(smem_u32(&sh.o_full[1]));
-                }
-                __syncwarp();
             }
             // the last MMAs are complete before shared and tensor memory are given back
+            if (elect_one()) umma_commit(smem_u32(&sh.drained));
+            __syncwarp();
+            mbar_wait_parity(smem_u32(&sh.drained), 0u);
+        } else if (warp == kC_WarpO) {
+            // ------------------------------------------------ O += P V, the same items
+            constexpr uint32_t kIdesc = umma_idesc(128, 128, true);
+            const uint32_t base = __shfl_sync(0xffffffffu, tmem, 0);
+            const int lbox = kTma ? a.log2box : 7;
+            // 16 tokens are two groups of 8 rows: next to one another in a box, or, of boxes of 8 rows, a box each
+            const uint32_t half_bytes = 128u << lbox, group_bytes = lbox == 3 ? 2048u : 1024u;
+            int slot = 0;
+            uint32_t phase = 0, p_phase = 0;              // p_phase: bit x of p_full[x]
+            bool ok = true;
+            while (ok && walk.next()) {
+                const bool split = walk.unit.split;
+                const int n = (walk.t1 - walk.t0) * (split ? 1 : 2);
+                for (int i = 0; i < n; ++i) {
+                    const int x = i & 1;
+                    if ((split || x == 0) && !(ok = wait(sh.v_full[slot], phase))) break;
+                    if (!(ok = wait(sh.p_full[x], p_phase >> x & 1u))) break;
+                    p_phase ^= 1u << x;
+                    tc_fence_after();
+                    if (elect_one()) {
+                        const uint32_t v0 = smem0 + kC_OffV + slot * kC_TileBytes;
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) {
+                            const uint32_t r = (uint32_t)k * 16, in_box = r & ((1u << lbox) - 1);
+                            const uint64_t vd = umma_desc_sw128(v0 + (r - in_box) * 256 + in_box * 128, half_bytes, group_bytes);
+                            umma_ts(base + kC_ColO + x * 128, base + kC_ColP + x * 64 + k * 8, vd, kIdesc, (i >= 2 || k) ? 1u : 0u);
+                        }
+                        umma_commit(smem_u32(&sh.o_done[x]));
+                        if (split || x == 1) umma_commit(smem_u32(&sh.v_empty[slot]));
+                    }
+                    __syncwarp();
+                    if ((split || x == 1) && ++slot == kC_SlotsV) { slot = 0; phase ^= 1; }
+                }
+            }
             if (elect_one()) umma_commit(smem_u32(&sh.drained));
             __syncwarp();
             mbar_wait_parity(smem_u32(&sh.drained), 0u);
@@ -510,9 +477,9 @@ __global__ void __launch_bounds__(kC_Threads, 1) chunk_attn_kernel(const __grid_
             asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kC_RegsSoftmax));
             const int x = warp >> 2, row = tid & 127;
             const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-            const uint32_t col_s = tmem + kC_ColS + x * 128 + lanes, col_o = tmem + kC_ColO + x * 128 + lanes;
+            const uint32_t col_s = tmem + kC_ColS + lanes, col_p = tmem + kC_ColP + x * 64 + lanes, col_o = tmem + kC_ColO + x * 128 + lanes;
             const float scale = a.scale_log2 > 0.0f ? a.scale_log2 : 1.0f;   // others are multiplied in beforehand
-            uint32_t s_phase = 0, j_phase = 0;
+            uint32_t items = 0, j_phase = 0;             // items of this row tile so far
             // all softmax threads have come this far (bounded, as a barrier of the hardware would not be)
             auto join = [&]() -> bool {
                 __syncwarp();
@@ -537,14 +504,16 @@ __global__ void __launch_bounds__(kC_Threads, 1) chunk_attn_kernel(const __grid_
                 bool any = false;                                        // O holds something
                 const int t0 = walk.t0, t1 = walk.t1;
                 for (int j = t0 + (split ? x : 0); j < t1; j += split ? 2 : 1) {
-                    if (!(ok = wait(sh.s_full[x], s_phase))) break;
-                    s_phase ^= 1;
+                    if (!(ok = wait(sh.s_full[x], items & 1u))) break;
+                    tc_fence_after();
                     if (!idle) {
-                        tc_fence_after();
-                        const int seen = limit - j * kChunkTile;         // columns below it are seen
-                        const bool mask = __any_sync(0xffffffffu, seen < kChunkTile);
                         float v[128];
                         load_scores(col_s, v);
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(smem_u32(&sh.s_free));
+                        const int seen = limit - j * kChunkTile;         // columns below it are seen
+                        const bool mask = __any_sync(0xffffffffu, seen < kChunkTile);
                         if (!(a.scale_log2 > 0.0f)) {
 #pragma unroll
                             for (int i = 0; i < 128; ++i) v[i] *= a.scale_log2;
@@ -563,6 +532,9 @@ __global__ void __launch_bounds__(kC_Threads, 1) chunk_attn_kernel(const __grid_
 #pragma unroll
                         for (int k = 0; k < 4; ++k) x4[k] = fmaxf(x4[k], v[124 + k]);
                         const float mx = max3(x4[0], x4[1], fmaxf(x4[2], x4[3])) * scale;
+                        // the last product is done with O and with P
+                        if (!(ok = items == 0 || wait(sh.o_done[x], (items - 1) & 1u))) break;
+                        tc_fence_after();
                         const bool raise = mx > m + kC_Raise || (m == -CUDART_INF_F && mx > m);
                         if (__any_sync(0xffffffffu, raise)) {
                             const float m_new = raise ? mx : m;
@@ -596,17 +568,22 @@ __global__ void __launch_bounds__(kC_Threads, 1) chunk_attn_kernel(const __grid_
                                 else add2(s0, s1, e0, e1);
                                 pk[i] = pack_bf16(e0, e1);
                             }
-                            tmem_st16(col_s + c * 16, pk);
+                            tmem_st16(col_p + c * 16, pk);
                         }
                         l += (s0 + s1) + (s2 + s3);
                         any = true;
                         tmem_wait_st();
                         tc_fence_before();
+                    } else {
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(smem_u32(&sh.s_free));
+                        if (!(ok = items == 0 || wait(sh.o_done[x], (items - 1) & 1u))) break;   // never ahead of the others by more than an item
                     }
                     __syncwarp();
                     if (lane == 0) mbar_arrive(smem_u32(&sh.p_full[x]));
+                    ++items;
                 }
-                if (!ok || !(ok = wait(sh.o_full[x], part & 1u))) break;
+                if (!ok || !(ok = items == 0 || wait(sh.o_done[x], (items - 1) & 1u))) break;
                 tc_fence_after();
 
                 // ---- join the halves, write the result or this part
@@ -766,10 +743,10 @@ static bool q_map(CUtensorMap *tm, TensorView q, int rows, int Hq, int log2g) {
     const cuuint32_t box[4] = {64u, 1u << log2g, (cuuint32_t)(kChunkTile >> log2g), 2u};
     return encode_map(tm, 4, q.ptr, dims, strides, box);
 }
-static bool pool_map(CUtensorMap *tm, TensorView T, int n_pages, int Hkv, int shift) {
+static bool pool_map(CUtensorMap *tm, TensorView T, int n_pages, int Hkv, int shift, int log2box, int halves) {
     const cuuint64_t dims[5] = {64u, 1ull << shift, 2u, (cuuint64_t)Hkv, (cuuint64_t)n_pages};
     const cuuint64_t strides[4] = {(cuuint64_t)T.sn * 2, 128u, (cuuint64_t)T.sh * 2, (cuuint64_t)T.sb * 2};
-    const cuuint32_t box[5] = {64u, shift < 7 ? 1u << shift : (cuuint32_t)kChunkTile, 1u, 1u, 1u};
+    const cuuint32_t box[5] = {64u, 1u << log2box, (cuuint32_t)halves, 1u, 1u};
     return encode_map(tm, 5, T.ptr, dims, strides, box);
 }
 
@@ -784,6 +761,7 @@ cudaError_t launch_chunk_attn(int B, int Hq, int Hkv, float sm_scale, TensorView
     a.log2g = 0;
     while ((Hkv << a.log2g) < Hq) ++a.log2g;
     a.max_ctas = kChunkMaxCtas;
+    a.log2box = shift < 7 ? shift : 7;
     a.scale_log2 = sm_scale * kLog2e;
     a.out = out; a.lse = lse;
     char *ws = reinterpret_cast<char *>(workspace);
@@ -795,7 +773,8 @@ cudaError_t launch_chunk_attn(int B, int Hq, int Hkv, float sm_scale, TensorView
     memset(&mq, 0, sizeof(mq));
     memset(&mk, 0, sizeof(mk));
     memset(&mv, 0, sizeof(mv));
-    const bool tma = shift >= 3 && q_map(&mq, q, n_rows, Hq, a.log2g) && pool_map(&mk, K, n_pages, Hkv, shift) && pool_map(&mv, V, n_pages, Hkv, shift);
+    const bool tma = shift >= 3 && q_map(&mq, q, n_rows, Hq, a.log2g) && pool_map(&mk, K, n_pages, Hkv, shift, a.log2box, 1) &&
+                     pool_map(&mv, V, n_pages, Hkv, shift, a.log2box, 2);
     cudaError_t e = cudaFuncSetAttribute(tma ? chunk_attn_kernel<true> : chunk_attn_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kC_Smem);
     if (e != cudaSuccess) return e;
     int grid = sm_count();
