@@ -76,7 +76,10 @@ struct ChunkShared {
     int last_part;
     uint32_t tmem;
     volatile int fail;
-    float ml[2][128][2];         // the halves' maxima and sums, where they share a unit
+    union {
+        float ml[2][128][2];     // the halves' maxima and sums, where they share a unit
+        float2 joined[kChunkRows];   // of the rows of a unit whose parts are joined: maximum, one over the sum
+    };
 };
 
 __device__ __forceinline__ float exp2_approx(float x) {
@@ -631,10 +634,10 @@ __global__ void __launch_bounds__(kC_Threads, 1) chunk_attn_kernel(const __grid_
                         }
                         if (!mine) continue;
                         if (walk.cut) {
-                            float4 *dst = reinterpret_cast<float4 *>(a.part_acc + ((long long)slot * kChunkRows + r) * kD + c * 32);
+                            float4 *dst = reinterpret_cast<float4 *>(a.part_acc) + ((long long)slot * (kD / 4) + c * 8) * kChunkRows + r;
 #pragma unroll
                             for (int i = 0; i < 8; ++i)
-                                __stcg(dst + i, make_float4(__uint_as_float(v[4 * i]), __uint_as_float(v[4 * i + 1]), __uint_as_float(v[4 * i + 2]), __uint_as_float(v[4 * i + 3])));
+                                __stcg(dst + i * kChunkRows, make_float4(__uint_as_float(v[4 * i]), __uint_as_float(v[4 * i + 1]), __uint_as_float(v[4 * i + 2]), __uint_as_float(v[4 * i + 3])));
                         } else {
                             uint4 *dst = reinterpret_cast<uint4 *>(a.out + out_row * kD + c * 32);
 #pragma unroll
@@ -655,6 +658,7 @@ __global__ void __launch_bounds__(kC_Threads, 1) chunk_attn_kernel(const __grid_
                     }
                 }
                 tc_fence_before();
+                bool settle = split;                     // both halves have read both O before the next unit's first product may write them
                 if (walk.cut) {
                     // ---- the last of the unit's parts joins them
                     __threadfence();
@@ -667,36 +671,56 @@ __global__ void __launch_bounds__(kC_Threads, 1) chunk_attn_kernel(const __grid_
                     }
                     if (!(ok = join())) break;
                     if (sh.last_part) {
-                        // slot 1 of the first CTA, slot 0 of the others; a thread takes four columns of a row
+                        settle = true;                   // ... or what the rows' threads share before the next unit's write it
+                        // slot 1 of the first CTA, slot 0 of the others
                         const long long s0 = (long long)walk.first_cta * 2 + 1, s1 = (long long)(walk.first_cta + 1) * 2;
                         const int np = walk.n_parts;
-                        for (int e = tid; e < n_rows * 32; e += kC_Softmax) {
-                            const int er = e >> 5, ec = (e & 31) * 4;
-                            auto at = [&](int k) -> long long { return (k == 0 ? s0 : s1 + 2 * (k - 1)) * kChunkRows + er; };
-                            float mm = -CUDART_INF_F;
-                            for (int k = 0; k < np; ++k) mm = fmaxf(mm, __ldcg(a.part_ml + at(k) * 2));
+                        auto slot_of = [&](int k) -> long long { return k == 0 ? s0 : s1 + 2 * (k - 1); };
+                        const float2 *ml = reinterpret_cast<const float2 *>(a.part_ml);
+                        // a row's maximum, and one over its sum, for the threads that share the row
+                        if (tid < n_rows) {
+                            float mm = -CUDART_INF_F, ll = 0.0f;
+#pragma unroll 4
+                            for (int k = 0; k < np; ++k) mm = fmaxf(mm, __ldcg(&ml[slot_of(k) * kChunkRows + tid]).x);
                             const float b = mm == -CUDART_INF_F ? 0.0f : mm;
-                            float ll = 0.0f;
-                            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
                             for (int k = 0; k < np; ++k) {
-                                const float2 ml = __ldcg(reinterpret_cast<const float2 *>(a.part_ml + at(k) * 2));
-                                const float4 v = __ldcg(reinterpret_cast<const float4 *>(a.part_acc + at(k) * kD + ec));
-                                const float w = exp2_approx(ml.x - b);
-                                ll = fmaf(ml.y, w, ll);
-                                acc.x = fmaf(v.x, w, acc.x); acc.y = fmaf(v.y, w, acc.y);
-                                acc.z = fmaf(v.z, w, acc.z); acc.w = fmaf(v.w, w, acc.w);
+                                const float2 v = __ldcg(&ml[slot_of(k) * kChunkRows + tid]);
+                                ll = fmaf(v.y, exp2_approx(v.x - b), ll);
                             }
-                            const float i = ll == 0.0f ? 0.0f : ll > 0.0f ? __frcp_rn(ll) : ll;
-                            const long long orow = ((long long)(walk.s.row0 + walk.unit.tok0 + (er >> a.log2g)) * a.Hkv + walk.h << a.log2g) + (er & ((1 << a.log2g) - 1));
-                            uint2 w = make_uint2(0u, 0u);
-                            if (ll != 0.0f) w = make_uint2(pack_bf16(acc.x * i, acc.y * i), pack_bf16(acc.z * i, acc.w * i));
-                            *reinterpret_cast<uint2 *>(a.out + orow * kD + ec) = w;
-                            if (ec == 0 && a.lse) a.lse[orow] = ll == 0.0f ? -CUDART_INF_F : (mm + log2f(ll)) * kLn2;
+                            sh.joined[tid] = make_float2(b, ll == 0.0f ? 0.0f : ll > 0.0f ? __frcp_rn(ll) : ll);
+                            if (a.lse) {
+                                const long long o = ((long long)(walk.s.row0 + walk.unit.tok0 + (tid >> a.log2g)) * a.Hkv + walk.h << a.log2g) + (tid & ((1 << a.log2g) - 1));
+                                a.lse[o] = ll == 0.0f ? -CUDART_INF_F : (mm + log2f(ll)) * kLn2;
+                            }
+                        }
+                        if (!(ok = join())) break;
+                        // a thread takes eight columns of a row at a time, and the loads of all parts (four at a time) together
+                        const int lrows = 32 - __clz(n_rows - 1 > 0 ? n_rows - 1 : 1), rows2 = 1 << lrows;   // rows, rounded up to a power of two
+                        for (int e = tid; e < 16 * rows2; e += kC_Softmax) {
+                            const int er = e & (rows2 - 1), ec = e >> lrows;
+                            if (er >= n_rows) continue;
+                            const float2 j = sh.joined[er];
+                            float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+                            for (int k = 0; k < np; ++k) {
+                                const long long sl = slot_of(k);
+                                const float4 *v = reinterpret_cast<const float4 *>(a.part_acc) + (sl * (kD / 4) + 2 * ec) * kChunkRows + er;
+                                const float4 v0 = __ldcg(v), v1 = __ldcg(v + kChunkRows);
+                                const float w = exp2_approx(__ldcg(&ml[sl * kChunkRows + er]).x - j.x);
+                                acc[0] = fmaf(v0.x, w, acc[0]); acc[1] = fmaf(v0.y, w, acc[1]); acc[2] = fmaf(v0.z, w, acc[2]); acc[3] = fmaf(v0.w, w, acc[3]);
+                                acc[4] = fmaf(v1.x, w, acc[4]); acc[5] = fmaf(v1.y, w, acc[5]); acc[6] = fmaf(v1.z, w, acc[6]); acc[7] = fmaf(v1.w, w, acc[7]);
+                            }
+                            const long long o = ((long long)(walk.s.row0 + walk.unit.tok0 + (er >> a.log2g)) * a.Hkv + walk.h << a.log2g) + (er & ((1 << a.log2g) - 1));
+                            uint4 w = make_uint4(0u, 0u, 0u, 0u);
+                            if (j.y != 0.0f)
+                                w = make_uint4(pack_bf16(acc[0] * j.y, acc[1] * j.y), pack_bf16(acc[2] * j.y, acc[3] * j.y),
+                                               pack_bf16(acc[4] * j.y, acc[5] * j.y), pack_bf16(acc[6] * j.y, acc[7] * j.y));
+                            *reinterpret_cast<uint4 *>(a.out + o * kD + ec * 8) = w;
                         }
                     }
                 }
-                if (split) ok = join();   // both halves have read both O before the next unit's first MMA may write them
+                if (settle) ok = join();
             }
         }
     }

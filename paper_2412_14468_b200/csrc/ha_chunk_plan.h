@@ -42,11 +42,12 @@ HA_HD ChunkSeq chunk_seq(int seq_len, int off0, int off1, int n_rows, int log2g,
     bad = off0 < 0 || off1 < off0 || off1 > n_rows;
     s.cnt = bad ? 0 : off1 - off0;
     const int t = chunk_tokens_per_unit(log2g);
-    s.units = (int)(((long long)s.cnt + t - 1) / t);
+    s.units = (int)(((long long)s.cnt + t - 1) >> (8 - log2g));
     return s;
 }
 
-HA_HD int chunk_tiles(long long hi) { return hi <= kChunkTile ? 1 : (int)((hi + kChunkTile - 1) / kChunkTile); }
+static_assert(kChunkRows == 256 && kChunkTile == 128, "shifts by 8 and 7 below");
+HA_HD int chunk_tiles(long long hi) { return hi <= kChunkTile ? 1 : (int)((hi + kChunkTile - 1) >> 7); }
 
 HA_HD ChunkUnit chunk_unit(const ChunkSeq &s, int u, int log2g, bool causal) {
     ChunkUnit r;
@@ -60,10 +61,15 @@ HA_HD ChunkUnit chunk_unit(const ChunkSeq &s, int u, int log2g, bool causal) {
     return r;
 }
 
-// sum over y = 1 .. x of floor(y / k)
-HA_HD long long chunk_floor_sum(long long x, int k) {
-    const long long t = x / k, r = x % k;
-    return k * (t * (t - 1) / 2) + t * (r + 1);
+// a / b for a >= 0, b > 0; most fit 32 bits, whose division takes a tenth of the time
+HA_HD long long chunk_div(long long a, long long b) {
+    return ((unsigned long long)(a | b) >> 32) == 0 ? (long long)((uint32_t)a / (uint32_t)b) : a / b;
+}
+
+// sum over y = 1 .. x of floor(y / 2^lk)
+HA_HD long long chunk_floor_sum(long long x, int lk) {
+    const long long t = x >> lk, r = x & ((1 << lk) - 1);
+    return ((t * (t - 1) / 2) << lk) + t * (r + 1);
 }
 
 // Cost of units 0 .. u - 1 of one KV head, all of them with all their tokens (u <= units, the last unit apart).
@@ -74,7 +80,7 @@ HA_HD long long chunk_cost_full_units(const ChunkSeq &s, int u, int log2g, bool 
     const long long a = (long long)s.n - s.cnt;     // tokens in front of the new ones; negative: units that see nothing cost one tile
     long long m = u, skipped = 0;
     if (a < 0) {                                    // units whose last position lies below 1 have one tile
-        skipped = (-a) / t;
+        skipped = (-a) >> (8 - log2g);
         if (skipped > m) skipped = m;
     }
     // unit i (counted from 1) sees a + i t tokens: ceil((a + i t) / 128) tiles
@@ -84,12 +90,13 @@ HA_HD long long chunk_cost_full_units(const ChunkSeq &s, int u, int log2g, bool 
     if (m == 0) return tiles * kChunkCostPair;
     if (t == 2 * kChunkTile) {
         // floor((base + 256 i) / 128) = floor(base / 128) + 2 i, base >= -255 + 127
-        const long long q = base >= 0 ? base / kChunkTile : -((-base + kChunkTile - 1) / kChunkTile);
+        const long long q = base >> 7;              // rounds down
         tiles += m * q + m * (m + 1);
     } else {
-        const int k = kChunkTile / t;               // floor((base + i t) / 128) = floor((floor(base / t) + i) / k)
-        const long long q = base / t;               // base > 127 - t >= -1
-        tiles += chunk_floor_sum(q + m, k) - chunk_floor_sum(q, k);
+        // k = 128 / t: floor((base + i t) / 128) = floor((floor(base / t) + i) / k)
+        const int lk = log2g - 1;
+        const long long q = base >> (8 - log2g);    // base > 127 - t >= -1
+        tiles += chunk_floor_sum(q + m, lk) - chunk_floor_sum(q, lk);
     }
     return tiles * kChunkCostPair;
 }
@@ -105,12 +112,12 @@ HA_HD int chunk_ctas(long long W, int most) {
     const long long c = W / kChunkCostMost;
     return c < 1 ? 1 : c < most ? (int)c : most;
 }
-HA_HD long long chunk_bound(long long W, int C, int c) { return W * c / C; }
-HA_HD int chunk_cta_of(long long W, int C, long long x) { return (int)(((x + 1) * C - 1) / W); }
+HA_HD long long chunk_bound(long long W, int C, int c) { return chunk_div(W * c, C); }
+HA_HD int chunk_cta_of(long long W, int C, long long x) { return (int)chunk_div((x + 1) * C - 1, W); }
 // first tile of a unit beginning at u0 that a stretch beginning at f takes
 HA_HD int chunk_first_tile(long long f, long long u0, int cost, int tiles) {
     if (f <= u0) return 0;
-    const long long t = (f - u0 + cost - 1) / cost;
+    const long long t = chunk_div(f - u0 + cost - 1, cost);
     return t < tiles ? (int)t : tiles;
 }
 
@@ -138,7 +145,7 @@ struct ChunkWalk {
         b = b_;
         load();
         const long long per_head = chunk_cost_head(s, log2g, causal);
-        h = (int)(rest / per_head);
+        h = (int)chunk_div(rest, per_head);
         rest -= h * per_head;
         int lo = 0, hi = s.units - 1;              // the last unit that begins at or before `rest`
         while (lo < hi) {
