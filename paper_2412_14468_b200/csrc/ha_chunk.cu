@@ -67,7 +67,18 @@ struct ChunkArgs {
     float *part_ml, *part_acc;   // [CTA][2][256] (m, l) and [CTA][2][256][128]
 };
 
+// What a CTA does next: written by the warp that fetches keys, read by all roles.
+struct ChunkPart {
+    int b, h, n, row, toks, first_pos, t0, t1;       // row: of q, the unit's first; toks: 0 behind the last part
+    int split, cut, first_cta, n_parts;
+};
+// Four places: the keys of a part are asked for when all scores of the last but one have been ordered, so that no role is more than
+// three parts behind.
+constexpr int kC_Parts = 4;
+
 struct ChunkShared {
+    ChunkPart parts[kC_Parts];
+    unsigned long long part_full[kC_Parts];
     unsigned long long k_full[kC_SlotsK], k_empty[kC_SlotsK], v_full[kC_SlotsV], v_empty[kC_SlotsV], q_full, q_empty;
     unsigned long long s_full[2], s_free, p_full[2], o_done[2], joint, drained;
     long long start_rest, total;
@@ -125,9 +136,10 @@ __device__ __forceinline__ void tma_load_q(uint32_t dst, const CUtensorMap *map,
 
 // The fetching warps: tiles of K (and q) or of V, in the order of the parts.  log2 of the rows of a box: the rows of a V tile lie box
 // by box, in either half of the columns; those of a K tile half by half.
-template <bool kTma, bool kV, typename Wait>
-__device__ __forceinline__ void chunk_fetch(const ChunkArgs &a, ChunkWalk &walk, const CUtensorMap *map, const CUtensorMap *map_q, ChunkShared &sh,
+template <bool kTma, bool kV, typename NextPart, typename Wait>
+__device__ __forceinline__ void chunk_fetch(const ChunkArgs &a, NextPart next_part, const CUtensorMap *map, const CUtensorMap *map_q, ChunkShared &sh,
                                             uint32_t smem0, int lane, Wait wait) {
+    ChunkPart now = {};
     constexpr int kSlots = kV ? kC_SlotsV : kC_SlotsK;
     const TensorView &T = kV ? a.V : a.K;
     unsigned long long *full = kV ? sh.v_full : sh.k_full, *empty = kV ? sh.v_empty : sh.k_empty;
@@ -154,8 +166,8 @@ __device__ __forceinline__ void chunk_fetch(const ChunkArgs &a, ChunkWalk &walk,
     auto fetch_pages = [&](int batch) {
         const int e = batch * 32 + lane;
         int page = -1;
-        if ((long long)e << a.shift < walk.s.n) {
-            page = __ldg(a.table + (long long)walk.b * a.bt_sb + e);
+        if ((long long)e << a.shift < now.n) {
+            page = __ldg(a.table + (long long)now.b * a.bt_sb + e);
             if (bad_page(page)) page = -1;
         }
         if (batch & 1) pages1 = page;
@@ -168,8 +180,8 @@ __device__ __forceinline__ void chunk_fetch(const ChunkArgs &a, ChunkWalk &walk,
         for (int g = 0; g < 4; ++g) {
             const int tok = j * kChunkTile + g * 32 + lane;
             row_pages[g] = -1;
-            if (tok < walk.s.n) {
-                row_pages[g] = __ldg(a.table + (long long)walk.b * a.bt_sb + (tok >> a.shift));
+            if (tok < now.n) {
+                row_pages[g] = __ldg(a.table + (long long)now.b * a.bt_sb + (tok >> a.shift));
                 if (bad_page(row_pages[g])) row_pages[g] = -1;
             }
         }
@@ -181,7 +193,7 @@ __device__ __forceinline__ void chunk_fetch(const ChunkArgs &a, ChunkWalk &walk,
             for (int i = 0; i < 16; ++i) {
                 const int r = g * 32 + 2 * i + hw, page = __shfl_sync(0xffffffffu, row_pages[g], 2 * i + hw);
                 const uint16_t *src = T.ptr + ch * 8;
-                if (page >= 0) src += (long long)page * T.sb + (long long)walk.h * T.sh + (long long)((j * kChunkTile + r) & mask) * T.sn;
+                if (page >= 0) src += (long long)page * T.sb + (long long)now.h * T.sh + (long long)((j * kChunkTile + r) & mask) * T.sn;
                 const uint32_t at = kV ? ((uint32_t)(r >> lbox) << lbox) * 256 + (uint32_t)(ch >> 3) * (128u << lbox) + (uint32_t)(r & ((1 << lbox) - 1)) * 128
                                        : (uint32_t)(ch >> 3) * kC_Half + (uint32_t)r * 128;
                 cp_async16(dst + at + (((ch & 7) ^ (r & 7)) << 4), src, page >= 0 ? 16u : 0u);
@@ -215,11 +227,11 @@ __device__ __forceinline__ void chunk_fetch(const ChunkArgs &a, ChunkWalk &walk,
             const int which = lane & ((1 << lboxes) - 1), half = lane >> lboxes, tok = j * kChunkTile + (which << lbox);
             const int batch = (j * kChunkTile >> a.shift) >> 5;
             const int page = __shfl_sync(0xffffffffu, batch & 1 ? pages1 : pages0, (tok >> a.shift) & 31);
-            const int left = walk.s.n - j * kChunkTile, there = left >= kChunkTile ? 1 << lboxes : (left + (1 << lbox) - 1) >> lbox;
+            const int left = now.n - j * kChunkTile, there = left >= kChunkTile ? 1 << lboxes : (left + (1 << lbox) - 1) >> lbox;
             if (lane == 0) mbar_expect_tx(bar, ((uint32_t)there << lbox) * 256);
             __syncwarp();
             if (which < there && half < (kV ? 1 : 2))
-                tma_load_rows(dst + ((uint32_t)which << lbox) * (kV ? 256 : 128) + (kV ? 0 : half * kC_Half), map, tok & mask, kV ? 0 : half, walk.h, page, bar);
+                tma_load_rows(dst + ((uint32_t)which << lbox) * (kV ? 256 : 128) + (kV ? 0 : half * kC_Half), map, tok & mask, kV ? 0 : half, now.h, page, bar);
             ++issued;
             if (pending >= 0) {
                 cp_async_wait<0>();
@@ -230,9 +242,9 @@ __device__ __forceinline__ void chunk_fetch(const ChunkArgs &a, ChunkWalk &walk,
         if (++slot == kSlots) { slot = 0; phase ^= 1; }
         return true;
     };
-    for (uint32_t part = 0; ok && walk.next(); ++part) {
-        const int t0 = walk.t0, t1 = walk.t1;
-        const bool tail = !kTma || (kV && (long long)t1 * kChunkTile > walk.s.n);
+    for (uint32_t part = 0; ok && (ok = next_part(part, now)) && now.toks > 0; ++part) {
+        const int t0 = now.t0, t1 = now.t1;
+        const bool tail = !kTma || (kV && (long long)t1 * kChunkTile > now.n);
         if (kTma) {
             ahead = (t0 * kChunkTile >> a.shift) >> 5;
             fetch_pages(ahead);
@@ -246,17 +258,17 @@ __device__ __forceinline__ void chunk_fetch(const ChunkArgs &a, ChunkWalk &walk,
                 announce();
             }
             if (!(ok = part == 0 || wait(sh.q_empty, (part - 1) & 1u))) break;
-            const int n_rows = walk.unit.toks << a.log2g, rows = n_rows <= kChunkTile ? kChunkTile : kChunkRows;
+            const int n_rows = now.toks << a.log2g, rows = n_rows <= kChunkTile ? kChunkTile : kChunkRows;
             if (kTma) {
                 if (elect_one()) {
                     mbar_expect_tx(smem_u32(&sh.q_full), rows * 256);
                     for (int x = 0; x < rows / kChunkTile; ++x)
-                        tma_load_q(smem0 + kC_OffQ + x * kC_TileBytes, map_q, walk.h << a.log2g,
-                                   walk.s.row0 + walk.unit.tok0 + x * (kChunkTile >> a.log2g), smem_u32(&sh.q_full));
+                        tma_load_q(smem0 + kC_OffQ + x * kC_TileBytes, map_q, now.h << a.log2g,
+                                   now.row + x * (kChunkTile >> a.log2g), smem_u32(&sh.q_full));
                 }
                 ++issued_q;
             } else {
-                const uint16_t *q = a.q + (long long)(walk.s.row0 + walk.unit.tok0) * a.q_sn + (long long)(walk.h << a.log2g) * a.q_sh + ch * 8;
+                const uint16_t *q = a.q + (long long)(now.row) * a.q_sn + (long long)(now.h << a.log2g) * a.q_sh + ch * 8;
 #pragma unroll 8
                 for (int r = hw; r < rows; r += 2) {
                     const bool in = r < n_rows;
@@ -294,6 +306,7 @@ __global__ void __launch_bounds__(kC_Threads, 1) chunk_attn_kernel(const __grid_
     const uint32_t smem0 = smem_u32(smem);
 
     if (tid == 0) {
+        for (int i = 0; i < kC_Parts; ++i) mbar_init(smem_u32(&sh.part_full[i]), 1);
         for (int i = 0; i < kC_SlotsK; ++i) {
             mbar_init(smem_u32(&sh.k_full[i]), 1);
             mbar_init(smem_u32(&sh.k_empty[i]), 1);
@@ -379,28 +392,53 @@ __global__ void __launch_bounds__(kC_Threads, 1) chunk_attn_kernel(const __grid_
     tc_fence_after();
     const uint32_t tmem = sh.tmem;
 
+    auto gave_up = [&]() -> bool {
+        sh.fail = 1;
+        if (a.status) atomicOr(a.status, HA_DEV_TIMEOUT);
+        return false;
+    };
     auto wait = [&](unsigned long long &bar, uint32_t parity) -> bool {
         const uint32_t at = smem_u32(&bar);
         if (mbar_test(at, parity)) return true;
-        if (!mbar_wait_parity(at, parity)) {
-            sh.fail = 1;
-            if (a.status) atomicOr(a.status, HA_DEV_TIMEOUT);
-            return false;
-        }
-        return sh.fail == 0;
+        return mbar_wait_parity(at, parity) ? sh.fail == 0 : gave_up();
+    };
+    auto wait_parked = [&](unsigned long long &bar, uint32_t parity) -> bool {   // where nobody waits for the waiter
+        const uint32_t at = smem_u32(&bar);
+        if (mbar_test(at, parity)) return true;
+        return mbar_wait_parity<0>(at, parity) ? sh.fail == 0 : gave_up();
     };
 
     if (warp >= kC_WarpS) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kC_RegsOther));
     if (busy && sh.start_b >= 0) {
-        ChunkWalk walk;
-        walk.W = W; walk.C = C; walk.log2g = a.log2g; walk.B = a.B; walk.Hkv = a.Hkv; walk.n_rows = a.n_rows; walk.causal = a.causal != 0;
-        walk.seq_lens = a.seq_lens; walk.offsets = a.offsets;
-        walk.begin(blockIdx.x, sh.start_b, sh.start_rest);
-
+        // the next part, by the warp that walks along the CTA's stretch, and by the others
+        auto given_part = [&](uint32_t part, ChunkPart &now) -> bool {
+            if (!wait(sh.part_full[part % kC_Parts], (part / kC_Parts) & 1u)) return false;
+            now = sh.parts[part % kC_Parts];
+            return true;
+        };
         if (warp == kC_WarpK) {
-            chunk_fetch<kTma, false>(a, walk, &map_k, &map_q, sh, smem0, lane, wait);
+            ChunkWalk walk;
+            walk.W = W; walk.C = C; walk.log2g = a.log2g; walk.B = a.B; walk.Hkv = a.Hkv; walk.n_rows = a.n_rows; walk.causal = a.causal != 0;
+            walk.seq_lens = a.seq_lens; walk.offsets = a.offsets;
+            walk.begin(blockIdx.x, sh.start_b, sh.start_rest);
+            auto walked_part = [&](uint32_t part, ChunkPart &now) -> bool {
+                now.toks = 0;
+                if (walk.next()) {
+                    now.b = walk.b; now.h = walk.h; now.n = walk.s.n;
+                    now.row = walk.s.row0 + walk.unit.tok0; now.toks = walk.unit.toks; now.first_pos = walk.unit.first_pos;
+                    now.t0 = walk.t0; now.t1 = walk.t1;
+                    now.split = walk.unit.split; now.cut = walk.cut; now.first_cta = walk.first_cta; now.n_parts = walk.n_parts;
+                }
+                if (lane == 0) {
+                    sh.parts[part % kC_Parts] = now;
+                    mbar_arrive(smem_u32(&sh.part_full[part % kC_Parts]));
+                }
+                __syncwarp();
+                return true;
+            };
+            chunk_fetch<kTma, false>(a, walked_part, &map_k, &map_q, sh, smem0, lane, wait_parked);
         } else if (warp == kC_WarpV) {
-            chunk_fetch<kTma, true>(a, walk, &map_v, &map_q, sh, smem0, lane, wait);
+            chunk_fetch<kTma, true>(a, given_part, &map_v, &map_q, sh, smem0, lane, wait_parked);
         } else if (warp == kC_WarpS) {
             // ------------------------------------------------ S = Q K^T.  Item i of a part is row tile i % 2 and key tile i / 2, or, of
             // a unit of one row tile, key tile i
@@ -409,9 +447,10 @@ __global__ void __launch_bounds__(kC_Threads, 1) chunk_attn_kernel(const __grid_
             int slot = 0;
             uint32_t phase = 0, before = 0;               // before: items so far
             bool ok = true;
-            for (uint32_t part = 0; ok && walk.next(); ++part) {
-                const bool split = walk.unit.split;
-                const int n = (walk.t1 - walk.t0) * (split ? 1 : 2);
+            ChunkPart now = {};
+            for (uint32_t part = 0; ok && (ok = given_part(part, now)) && now.toks > 0; ++part) {
+                const bool split = now.split;
+                const int n = (now.t1 - now.t0) * (split ? 1 : 2);
                 if (!(ok = wait(sh.q_full, part & 1u))) break;
                 for (int i = 0; i < n; ++i, ++before) {
                     const int x = i & 1;
@@ -448,9 +487,10 @@ __global__ void __launch_bounds__(kC_Threads, 1) chunk_attn_kernel(const __grid_
             int slot = 0;
             uint32_t phase = 0, p_phase = 0;              // p_phase: bit x of p_full[x]
             bool ok = true;
-            while (ok && walk.next()) {
-                const bool split = walk.unit.split;
-                const int n = (walk.t1 - walk.t0) * (split ? 1 : 2);
+            ChunkPart now = {};
+            for (uint32_t part = 0; ok && (ok = given_part(part, now)) && now.toks > 0; ++part) {
+                const bool split = now.split;
+                const int n = (now.t1 - now.t0) * (split ? 1 : 2);
                 for (int i = 0; i < n; ++i) {
                     const int x = i & 1;
                     if ((split || x == 0) && !(ok = wait(sh.v_full[slot], phase))) break;
@@ -492,20 +532,23 @@ __global__ void __launch_bounds__(kC_Threads, 1) chunk_attn_kernel(const __grid_
                 return all;
             };
             bool ok = true;
-            for (uint32_t part = 0; ok && walk.next(); ++part) {
-                const bool split = walk.unit.split;
-                const int n_rows = walk.unit.toks << a.log2g;
+            for (uint32_t part = 0; ok; ++part) {
+                if (!(ok = wait(sh.part_full[part % kC_Parts], (part / kC_Parts) & 1u))) break;
+                const volatile ChunkPart &now = sh.parts[part % kC_Parts];   // read where it is needed: registers are for scores
+                if (now.toks == 0) break;
+                const bool split = now.split;
+                const int n_rows = now.toks << a.log2g;
                 const int r = split ? row : x * 128 + row;               // row of the unit
                 const bool idle = ((split ? 0 : x * 128) + (warp & 3) * 32) >= n_rows;   // no row of this warp exists
                 const int rc = r < n_rows ? r : n_rows - 1;              // rows that do not exist follow the last that does
-                int limit = walk.s.n;                                    // tokens below it are seen
+                int limit = now.n;                                    // tokens below it are seen
                 if (a.causal) {
-                    limit = walk.unit.first_pos + (rc >> a.log2g) + 1;
+                    limit = now.first_pos + (rc >> a.log2g) + 1;
                     if (limit < 0) limit = 0;
                 }
                 float m = -CUDART_INF_F, l = 0.0f;
                 bool any = false;                                        // O holds something
-                const int t0 = walk.t0, t1 = walk.t1;
+                const int t0 = now.t0, t1 = now.t1;
                 for (int j = t0 + (split ? x : 0); j < t1; j += split ? 2 : 1) {
                     if (!(ok = wait(sh.s_full[x], items & 1u))) break;
                     tc_fence_after();
@@ -609,8 +652,8 @@ __global__ void __launch_bounds__(kC_Threads, 1) chunk_attn_kernel(const __grid_
                 // half x of a split unit writes columns 64 x .. 64 x + 63 of the joined row; a row tile of its own all 128
                 const int c_lo = split ? 2 * x : 0, c_hi = split ? 2 * x + 2 : 4;
                 const bool mine = r < n_rows;
-                const long long out_row = ((long long)(walk.s.row0 + walk.unit.tok0 + (r >> a.log2g)) * a.Hkv + walk.h << a.log2g) + (r & ((1 << a.log2g) - 1));
-                const int slot = (int)blockIdx.x * 2 + (walk.cut && blockIdx.x == walk.first_cta ? 1 : 0);
+                const long long out_row = ((long long)(now.row + (r >> a.log2g)) * a.Hkv + now.h << a.log2g) + (r & ((1 << a.log2g) - 1));
+                const int slot = (int)blockIdx.x * 2 + (now.cut && blockIdx.x == now.first_cta ? 1 : 0);
                 const float inv = l > 0.0f ? __frcp_rn(l) : l == 0.0f ? 0.0f : l;   // nothing seen: 0; NaN stays
                 if (!idle) {
 #pragma unroll
@@ -633,7 +676,7 @@ __global__ void __launch_bounds__(kC_Threads, 1) chunk_attn_kernel(const __grid_
                             }
                         }
                         if (!mine) continue;
-                        if (walk.cut) {
+                        if (now.cut) {
                             float4 *dst = reinterpret_cast<float4 *>(a.part_acc) + ((long long)slot * (kD / 4) + c * 8) * kChunkRows + r;
 #pragma unroll
                             for (int i = 0; i < 8; ++i)
@@ -651,7 +694,7 @@ __global__ void __launch_bounds__(kC_Threads, 1) chunk_attn_kernel(const __grid_
                         }
                     }
                     if (mine && (!split || x == 0)) {
-                        if (walk.cut)
+                        if (now.cut)
                             __stcg(reinterpret_cast<float2 *>(a.part_ml + ((long long)slot * kChunkRows + r) * 2), make_float2(m, l));
                         else if (a.lse)
                             a.lse[out_row] = l == 0.0f ? -CUDART_INF_F : (m + log2f(l)) * kLn2;
@@ -659,22 +702,22 @@ __global__ void __launch_bounds__(kC_Threads, 1) chunk_attn_kernel(const __grid_
                 }
                 tc_fence_before();
                 bool settle = split;                     // both halves have read both O before the next unit's first product may write them
-                if (walk.cut) {
+                if (now.cut) {
                     // ---- the last of the unit's parts joins them
                     __threadfence();
                     if (!(ok = join())) break;
                     if (tid == 0) {
-                        const int seen = atomicAdd(a.tickets + walk.first_cta, 1);
-                        sh.last_part = seen == walk.n_parts - 1;
-                        if (sh.last_part) a.tickets[walk.first_cta] = 0;
+                        const int seen = atomicAdd(a.tickets + now.first_cta, 1);
+                        sh.last_part = seen == now.n_parts - 1;
+                        if (sh.last_part) a.tickets[now.first_cta] = 0;
                         __threadfence();
                     }
                     if (!(ok = join())) break;
                     if (sh.last_part) {
                         settle = true;                   // ... or what the rows' threads share before the next unit's write it
                         // slot 1 of the first CTA, slot 0 of the others
-                        const long long s0 = (long long)walk.first_cta * 2 + 1, s1 = (long long)(walk.first_cta + 1) * 2;
-                        const int np = walk.n_parts;
+                        const long long s0 = (long long)now.first_cta * 2 + 1, s1 = (long long)(now.first_cta + 1) * 2;
+                        const int np = now.n_parts;
                         auto slot_of = [&](int k) -> long long { return k == 0 ? s0 : s1 + 2 * (k - 1); };
                         const float2 *ml = reinterpret_cast<const float2 *>(a.part_ml);
                         // a row's maximum, and one over its sum, for the threads that share the row
@@ -690,33 +733,58 @@ __global__ void __launch_bounds__(kC_Threads, 1) chunk_attn_kernel(const __grid_
                             }
                             sh.joined[tid] = make_float2(b, ll == 0.0f ? 0.0f : ll > 0.0f ? __frcp_rn(ll) : ll);
                             if (a.lse) {
-                                const long long o = ((long long)(walk.s.row0 + walk.unit.tok0 + (tid >> a.log2g)) * a.Hkv + walk.h << a.log2g) + (tid & ((1 << a.log2g) - 1));
+                                const long long o = ((long long)(now.row + (tid >> a.log2g)) * a.Hkv + now.h << a.log2g) + (tid & ((1 << a.log2g) - 1));
                                 a.lse[o] = ll == 0.0f ? -CUDART_INF_F : (mm + log2f(ll)) * kLn2;
                             }
                         }
                         if (!(ok = join())) break;
-                        // a thread takes eight columns of a row at a time, and the loads of all parts (four at a time) together
+                        // a thread takes four pieces of eight columns of a row at a time, the loads of a part's all in flight
                         const int lrows = 32 - __clz(n_rows - 1 > 0 ? n_rows - 1 : 1), rows2 = 1 << lrows;   // rows, rounded up to a power of two
-                        for (int e = tid; e < 16 * rows2; e += kC_Softmax) {
-                            const int er = e & (rows2 - 1), ec = e >> lrows;
-                            if (er >= n_rows) continue;
-                            const float2 j = sh.joined[er];
-                            float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
+                        for (int e0 = tid; e0 < 16 * rows2; e0 += 4 * kC_Softmax) {
+                            float acc[4][8];
+#pragma unroll
+                            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) acc[u][i] = 0.0f;
                             for (int k = 0; k < np; ++k) {
                                 const long long sl = slot_of(k);
-                                const float4 *v = reinterpret_cast<const float4 *>(a.part_acc) + (sl * (kD / 4) + 2 * ec) * kChunkRows + er;
-                                const float4 v0 = __ldcg(v), v1 = __ldcg(v + kChunkRows);
-                                const float w = exp2_approx(__ldcg(&ml[sl * kChunkRows + er]).x - j.x);
-                                acc[0] = fmaf(v0.x, w, acc[0]); acc[1] = fmaf(v0.y, w, acc[1]); acc[2] = fmaf(v0.z, w, acc[2]); acc[3] = fmaf(v0.w, w, acc[3]);
-                                acc[4] = fmaf(v1.x, w, acc[4]); acc[5] = fmaf(v1.y, w, acc[5]); acc[6] = fmaf(v1.z, w, acc[6]); acc[7] = fmaf(v1.w, w, acc[7]);
+                                float4 v[4][2];
+                                float mk[4];
+#pragma unroll
+                                for (int u = 0; u < 4; ++u) {
+                                    const int e = e0 + u * kC_Softmax, er = e & (rows2 - 1), ec = e >> lrows;
+                                    if (ec >= 16 || er >= n_rows) continue;
+                                    const float4 *src = reinterpret_cast<const float4 *>(a.part_acc) + (sl * (kD / 4) + 2 * ec) * kChunkRows + er;
+                                    v[u][0] = __ldcg(src);
+                                    v[u][1] = __ldcg(src + kChunkRows);
+                                    mk[u] = __ldcg(&ml[sl * kChunkRows + er]).x;
+                                }
+#pragma unroll
+                                for (int u = 0; u < 4; ++u) {
+                                    const int e = e0 + u * kC_Softmax, er = e & (rows2 - 1);
+                                    if ((e >> lrows) >= 16 || er >= n_rows) continue;
+                                    const float w = exp2_approx(mk[u] - sh.joined[er].x);
+#pragma unroll
+                                    for (int i = 0; i < 2; ++i) {
+                                        acc[u][4 * i] = fmaf(v[u][i].x, w, acc[u][4 * i]);
+                                        acc[u][4 * i + 1] = fmaf(v[u][i].y, w, acc[u][4 * i + 1]);
+                                        acc[u][4 * i + 2] = fmaf(v[u][i].z, w, acc[u][4 * i + 2]);
+                                        acc[u][4 * i + 3] = fmaf(v[u][i].w, w, acc[u][4 * i + 3]);
+                                    }
+                                }
                             }
-                            const long long o = ((long long)(walk.s.row0 + walk.unit.tok0 + (er >> a.log2g)) * a.Hkv + walk.h << a.log2g) + (er & ((1 << a.log2g) - 1));
-                            uint4 w = make_uint4(0u, 0u, 0u, 0u);
-                            if (j.y != 0.0f)
-                                w = make_uint4(pack_bf16(acc[0] * j.y, acc[1] * j.y), pack_bf16(acc[2] * j.y, acc[3] * j.y),
-                                               pack_bf16(acc[4] * j.y, acc[5] * j.y), pack_bf16(acc[6] * j.y, acc[7] * j.y));
-                            *reinterpret_cast<uint4 *>(a.out + o * kD + ec * 8) = w;
+#pragma unroll
+                            for (int u = 0; u < 4; ++u) {
+                                const int e = e0 + u * kC_Softmax, er = e & (rows2 - 1), ec = e >> lrows;
+                                if (ec >= 16 || er >= n_rows) continue;
+                                const float inv = sh.joined[er].y;
+                                const long long o = ((long long)(now.row + (er >> a.log2g)) * a.Hkv + now.h << a.log2g) + (er & ((1 << a.log2g) - 1));
+                                uint4 w = make_uint4(0u, 0u, 0u, 0u);
+                                if (inv != 0.0f)
+                                    w = make_uint4(pack_bf16(acc[u][0] * inv, acc[u][1] * inv), pack_bf16(acc[u][2] * inv, acc[u][3] * inv),
+                                                   pack_bf16(acc[u][4] * inv, acc[u][5] * inv), pack_bf16(acc[u][6] * inv, acc[u][7] * inv));
+                                *reinterpret_cast<uint4 *>(a.out + o * kD + ec * 8) = w;
+                            }
                         }
                     }
                 }
