@@ -49,6 +49,7 @@ constexpr int kC_Half = kC_TileBytes / 2;
 constexpr int kC_SlotsK = 2, kC_SlotsV = 3;
 constexpr int kC_OffQ = 0, kC_OffK = 2 * kC_TileBytes, kC_OffV = kC_OffK + kC_SlotsK * kC_TileBytes;
 constexpr int kC_Smem = kC_OffV + kC_SlotsV * kC_TileBytes;   // 229376
+constexpr int kC_WarpPlan = 128;                   // sequences up to which one warp finds its CTA's share
 constexpr float kC_Raise = 8.0f;                   // how far (log2) a maximum may lie above the one that is referred to
 constexpr uint32_t kC_ColO = 0, kC_ColS = 256, kC_ColP = 384;   // tensor-memory columns: O0, O1, S, P0, P1
 
@@ -81,7 +82,7 @@ struct ChunkShared {
     unsigned long long part_full[kC_Parts];
     unsigned long long k_full[kC_SlotsK], k_empty[kC_SlotsK], v_full[kC_SlotsV], v_empty[kC_SlotsV], q_full, q_empty;
     unsigned long long s_full[2], s_free, p_full[2], o_done[2], joint, drained;
-    long long start_rest, total;
+    long long start_rest;
     long long warp_sums[kC_Threads / 32];
     int start_b;
     int last_part;
@@ -336,7 +337,8 @@ __global__ void __launch_bounds__(kC_Threads, 1) chunk_attn_kernel(const __grid_
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
 
-    // ---- the whole work, and where this CTA's share of it begins
+    // ---- the whole work, and where this CTA's share of it begins: needed by the warp that walks along it, and found by that warp
+    // alone (for up to kC_WarpPlan sequences) or by all of them
     auto cost_of = [&](int b, bool report) -> long long {
         if (b >= a.B) return 0;
         bool bad;
@@ -344,47 +346,76 @@ __global__ void __launch_bounds__(kC_Threads, 1) chunk_attn_kernel(const __grid_
         if (bad && report && a.status) atomicOr(a.status, HA_DEV_BAD_INDEX);
         return a.Hkv * chunk_cost_head(s, a.log2g, a.causal);
     };
-    // sum over the block and, in `before`, over the threads in front of this one
-    auto block_sum = [&](long long v, long long &before) -> long long {
+    auto ctas_for = [&](long long work) -> int { return chunk_ctas(work, a.max_ctas < (int)gridDim.x ? a.max_ctas : (int)gridDim.x); };
+    // of a warp: values in front of this lane's, and all of them
+    auto warp_sum = [&](long long v, long long &all) -> long long {
         long long x = v;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
             const long long y = __shfl_up_sync(0xffffffffu, x, d);
             if (lane >= d) x += y;
         }
-        __syncthreads();
-        if (lane == 31) sh.warp_sums[warp] = x;
-        __syncthreads();
-        long long base = 0, all = 0;
-        for (int w = 0; w < kC_Threads / 32; ++w) {
-            if (w < warp) base += sh.warp_sums[w];
-            all += sh.warp_sums[w];
-        }
-        before = base + x - v;
-        return all;
+        all = __shfl_sync(0xffffffffu, x, 31);
+        return x - v;
     };
-    long long W = 0, before = 0, mine = 0;
-    for (int b0 = 0; b0 < a.B; b0 += kC_Threads) {
-        mine = cost_of(b0 + tid, blockIdx.x == 0);
-        W += block_sum(mine, before);
-    }
-    const int C = chunk_ctas(W, a.max_ctas < (int)gridDim.x ? a.max_ctas : (int)gridDim.x);
-    const bool busy = W > 0 && (int)blockIdx.x < C;
-    if (busy) {
-        const long long f0 = chunk_bound(W, C, blockIdx.x);
-        long long done = 0;
-        for (int b0 = 0; b0 < a.B; b0 += kC_Threads) {
-            long long all = W;
-            if (a.B > kC_Threads) {
-                mine = cost_of(b0 + tid, false);
-                all = block_sum(mine, before);
+    long long W = 0, rest = 0;       // rest: how far into sequence `first_b` the share begins
+    int C = 1, first_b = -1;
+    if (a.B <= kC_WarpPlan) {
+        if (warp == kC_WarpK) {
+            long long cost[kC_WarpPlan / 32], before[kC_WarpPlan / 32];
+#pragma unroll
+            for (int i = 0; i < kC_WarpPlan / 32; ++i) cost[i] = cost_of(i * 32 + lane, blockIdx.x == 0);
+#pragma unroll
+            for (int i = 0; i < kC_WarpPlan / 32; ++i) {
+                long long all;
+                before[i] = W + warp_sum(cost[i], all);
+                W += all;
             }
-            const long long first = done + before;
-            if (first <= f0 && f0 < first + mine) {
-                sh.start_b = b0 + tid;
-                sh.start_rest = f0 - first;
+            C = ctas_for(W);
+            if (W > 0 && (int)blockIdx.x < C) {
+                const long long f0 = chunk_bound(W, C, blockIdx.x);
+#pragma unroll
+                for (int i = 0; i < kC_WarpPlan / 32; ++i) {
+                    const uint32_t m = __ballot_sync(0xffffffffu, before[i] <= f0 && f0 < before[i] + cost[i]);
+                    if (m) {
+                        const int l = __ffs(m) - 1;
+                        first_b = i * 32 + l;
+                        rest = f0 - __shfl_sync(0xffffffffu, before[i], l);
+                    }
+                }
             }
-            done += all;
+        }
+    } else {
+        auto block_sum = [&](long long v, long long &before) -> long long {
+            long long mine;
+            before = warp_sum(v, mine);
+            __syncthreads();
+            if (lane == 0) sh.warp_sums[warp] = mine;
+            __syncthreads();
+            long long all = 0;
+            for (int w = 0; w < kC_Threads / 32; ++w) {
+                if (w < warp) before += sh.warp_sums[w];
+                all += sh.warp_sums[w];
+            }
+            return all;
+        };
+        long long before = 0;
+        for (int b0 = 0; b0 < a.B; b0 += kC_Threads) W += block_sum(cost_of(b0 + tid, blockIdx.x == 0), before);
+        C = ctas_for(W);
+        if (W > 0 && (int)blockIdx.x < C) {
+            const long long f0 = chunk_bound(W, C, blockIdx.x);
+            long long done = 0;
+            for (int b0 = 0; b0 < a.B; b0 += kC_Threads) {
+                const long long mine = cost_of(b0 + tid, false), all = block_sum(mine, before), first = done + before;
+                if (first <= f0 && f0 < first + mine) {
+                    sh.start_b = b0 + tid;
+                    sh.start_rest = f0 - first;
+                }
+                done += all;
+            }
+            __syncthreads();
+            first_b = sh.start_b;
+            rest = sh.start_rest;
         }
     }
     tc_fence_before();
@@ -409,7 +440,7 @@ __global__ void __launch_bounds__(kC_Threads, 1) chunk_attn_kernel(const __grid_
     };
 
     if (warp >= kC_WarpS) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kC_RegsOther));
-    if (busy && sh.start_b >= 0) {
+    {
         // the next part, by the warp that walks along the CTA's stretch, and by the others
         auto given_part = [&](uint32_t part, ChunkPart &now) -> bool {
             if (!wait(sh.part_full[part % kC_Parts], (part / kC_Parts) & 1u)) return false;
@@ -418,12 +449,13 @@ __global__ void __launch_bounds__(kC_Threads, 1) chunk_attn_kernel(const __grid_
         };
         if (warp == kC_WarpK) {
             ChunkWalk walk;
+            const bool busy = first_b >= 0;
             walk.W = W; walk.C = C; walk.log2g = a.log2g; walk.B = a.B; walk.Hkv = a.Hkv; walk.n_rows = a.n_rows; walk.causal = a.causal != 0;
             walk.seq_lens = a.seq_lens; walk.offsets = a.offsets;
-            walk.begin(blockIdx.x, sh.start_b, sh.start_rest);
+            if (busy) walk.begin(blockIdx.x, first_b, rest);
             auto walked_part = [&](uint32_t part, ChunkPart &now) -> bool {
                 now.toks = 0;
-                if (walk.next()) {
+                if (busy && walk.next()) {
                     now.b = walk.b; now.h = walk.h; now.n = walk.s.n;
                     now.row = walk.s.row0 + walk.unit.tok0; now.toks = walk.unit.toks; now.first_pos = walk.unit.first_pos;
                     now.t0 = walk.t0; now.t1 = walk.t1;
@@ -683,13 +715,18 @@ __global__ void __launch_bounds__(kC_Threads, 1) chunk_attn_kernel(const __grid_
                                 __stcg(dst + i * kChunkRows, make_float4(__uint_as_float(v[4 * i]), __uint_as_float(v[4 * i + 1]), __uint_as_float(v[4 * i + 2]), __uint_as_float(v[4 * i + 3])));
                         } else {
                             uint4 *dst = reinterpret_cast<uint4 *>(a.out + out_row * kD + c * 32);
+                            uint32_t w[16];
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                uint32_t w[4];
+                            for (int i = 0; i < 16; ++i)
+                                w[i] = l == 0.0f ? 0u : pack_bf16(__uint_as_float(v[2 * i]) * inv, __uint_as_float(v[2 * i + 1]) * inv);
+                            if ((reinterpret_cast<uintptr_t>(a.out) & 31) == 0) {   // whole sectors of 32 bytes
 #pragma unroll
-                                for (int k = 0; k < 4; ++k)
-                                    w[k] = l == 0.0f ? 0u : pack_bf16(__uint_as_float(v[8 * i + 2 * k]) * inv, __uint_as_float(v[8 * i + 2 * k + 1]) * inv);
-                                dst[i] = make_uint4(w[0], w[1], w[2], w[3]);
+                                for (int i = 0; i < 2; ++i)
+                                    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst + 2 * i), "r"(w[8 * i]), "r"(w[8 * i + 1]),
+                                                 "r"(w[8 * i + 2]), "r"(w[8 * i + 3]), "r"(w[8 * i + 4]), "r"(w[8 * i + 5]), "r"(w[8 * i + 6]), "r"(w[8 * i + 7]) : "memory");
+                            } else {
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) dst[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
                             }
                         }
                     }
