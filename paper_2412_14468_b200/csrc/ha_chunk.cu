@@ -34,6 +34,7 @@
 #include "ha_umma.cuh"
 
 #include <cstring>
+#include <type_traits>
 #include <cuda.h>   // CUtensorMap (types only; the encoder is fetched through the runtime)
 
 namespace ha {
@@ -758,7 +759,32 @@ __global__ void __launch_bounds__(kC_Threads, 1) chunk_attn_kernel(const __grid_
                         auto slot_of = [&](int k) -> long long { return k == 0 ? s0 : s1 + 2 * (k - 1); };
                         const float2 *ml = reinterpret_cast<const float2 *>(a.part_ml);
                         // a row's maximum, and one over its sum, for the threads that share the row
-                        if (tid < n_rows) {
+                        auto row_of = [&](int er) -> long long {
+                            return ((long long)(now.row + (er >> a.log2g)) * a.Hkv + now.h << a.log2g) + (er & ((1 << a.log2g) - 1));
+                        };
+                        auto put = [&](int er, float mm, float b, float ll) {
+                            sh.joined[er] = make_float2(b, ll == 0.0f ? 0.0f : ll > 0.0f ? __frcp_rn(ll) : ll);
+                            if (a.lse) a.lse[row_of(er)] = ll == 0.0f ? -CUDART_INF_F : (mm + log2f(ll)) * kLn2;
+                        };
+                        if (n_rows <= 32) {            // few rows, which may have many parts: a lane for each part
+                            for (int er = warp; er < n_rows; er += kC_Softmax / 32) {
+                                float mm = -CUDART_INF_F, ll = 0.0f;
+                                for (int k = lane; k < np; k += 32) {
+                                    const float2 v = __ldcg(&ml[slot_of(k) * kChunkRows + er]);
+                                    const float m_new = fmaxf(mm, v.x), base = m_new == -CUDART_INF_F ? 0.0f : m_new;
+                                    ll = fmaf(ll, exp2_approx(mm - base), v.y * exp2_approx(v.x - base));
+                                    mm = m_new;
+                                }
+                                float top = mm;
+#pragma unroll
+                                for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+                                const float b = top == -CUDART_INF_F ? 0.0f : top;
+                                ll *= exp2_approx(mm - b);
+#pragma unroll
+                                for (int d = 16; d > 0; d >>= 1) ll += __shfl_xor_sync(0xffffffffu, ll, d);
+                                if (lane == 0) put(er, top, b, ll);
+                            }
+                        } else if (tid < n_rows) {
                             float mm = -CUDART_INF_F, ll = 0.0f;
 #pragma unroll 4
                             for (int k = 0; k < np; ++k) mm = fmaxf(mm, __ldcg(&ml[slot_of(k) * kChunkRows + tid]).x);
@@ -768,61 +794,68 @@ __global__ void __launch_bounds__(kC_Threads, 1) chunk_attn_kernel(const __grid_
                                 const float2 v = __ldcg(&ml[slot_of(k) * kChunkRows + tid]);
                                 ll = fmaf(v.y, exp2_approx(v.x - b), ll);
                             }
-                            sh.joined[tid] = make_float2(b, ll == 0.0f ? 0.0f : ll > 0.0f ? __frcp_rn(ll) : ll);
-                            if (a.lse) {
-                                const long long o = ((long long)(now.row + (tid >> a.log2g)) * a.Hkv + now.h << a.log2g) + (tid & ((1 << a.log2g) - 1));
-                                a.lse[o] = ll == 0.0f ? -CUDART_INF_F : (mm + log2f(ll)) * kLn2;
-                            }
+                            put(tid, mm, b, ll);
                         }
                         if (!(ok = join())) break;
-                        // a thread takes four pieces of eight columns of a row at a time, the loads of a part's all in flight
+                        // A thread takes kU pieces of eight columns of a row at a time, and kK parts of them: all of those loads are in flight
                         const int lrows = 32 - __clz(n_rows - 1 > 0 ? n_rows - 1 : 1), rows2 = 1 << lrows;   // rows, rounded up to a power of two
-                        for (int e0 = tid; e0 < 16 * rows2; e0 += 4 * kC_Softmax) {
-                            float acc[4][8];
+                        auto join_parts = [&](auto u_, auto k_) {
+                            constexpr int kU = decltype(u_)::value, kK = decltype(k_)::value;
+                            for (int e0 = tid; e0 < 16 * rows2; e0 += kU * kC_Softmax) {
+                                float acc[kU][8];
 #pragma unroll
-                            for (int u = 0; u < 4; ++u)
+                                for (int u = 0; u < kU; ++u)
 #pragma unroll
-                                for (int i = 0; i < 8; ++i) acc[u][i] = 0.0f;
-                            for (int k = 0; k < np; ++k) {
-                                const long long sl = slot_of(k);
-                                float4 v[4][2];
-                                float mk[4];
+                                    for (int i = 0; i < 8; ++i) acc[u][i] = 0.0f;
+                                for (int k0 = 0; k0 < np; k0 += kK) {
+                                    float4 v[kU][kK][2];
+                                    float mk[kU][kK];
 #pragma unroll
-                                for (int u = 0; u < 4; ++u) {
-                                    const int e = e0 + u * kC_Softmax, er = e & (rows2 - 1), ec = e >> lrows;
-                                    if (ec >= 16 || er >= n_rows) continue;
-                                    const float4 *src = reinterpret_cast<const float4 *>(a.part_acc) + (sl * (kD / 4) + 2 * ec) * kChunkRows + er;
-                                    v[u][0] = __ldcg(src);
-                                    v[u][1] = __ldcg(src + kChunkRows);
-                                    mk[u] = __ldcg(&ml[sl * kChunkRows + er]).x;
-                                }
+                                    for (int u = 0; u < kU; ++u) {
+                                        const int e = e0 + u * kC_Softmax, er = e & (rows2 - 1), ec = e >> lrows;
 #pragma unroll
-                                for (int u = 0; u < 4; ++u) {
-                                    const int e = e0 + u * kC_Softmax, er = e & (rows2 - 1);
-                                    if ((e >> lrows) >= 16 || er >= n_rows) continue;
-                                    const float w = exp2_approx(mk[u] - sh.joined[er].x);
+                                        for (int k = 0; k < kK; ++k) {
+                                            v[u][k][0] = v[u][k][1] = make_float4(0.f, 0.f, 0.f, 0.f);
+                                            mk[u][k] = -CUDART_INF_F;
+                                            if (ec >= 16 || er >= n_rows || k0 + k >= np) continue;
+                                            const long long sl = slot_of(k0 + k);
+                                            const float4 *src = reinterpret_cast<const float4 *>(a.part_acc) + (sl * (kD / 4) + 2 * ec) * kChunkRows + er;
+                                            v[u][k][0] = __ldcg(src);
+                                            v[u][k][1] = __ldcg(src + kChunkRows);
+                                            mk[u][k] = __ldcg(&ml[sl * kChunkRows + er]).x;
+                                        }
+                                    }
 #pragma unroll
-                                    for (int i = 0; i < 2; ++i) {
-                                        acc[u][4 * i] = fmaf(v[u][i].x, w, acc[u][4 * i]);
-                                        acc[u][4 * i + 1] = fmaf(v[u][i].y, w, acc[u][4 * i + 1]);
-                                        acc[u][4 * i + 2] = fmaf(v[u][i].z, w, acc[u][4 * i + 2]);
-                                        acc[u][4 * i + 3] = fmaf(v[u][i].w, w, acc[u][4 * i + 3]);
+                                    for (int u = 0; u < kU; ++u) {
+                                        const float b = sh.joined[(e0 + u * kC_Softmax) & (rows2 - 1)].x;
+#pragma unroll
+                                        for (int k = 0; k < kK; ++k) {
+                                            const float w = exp2_approx(mk[u][k] - b);
+#pragma unroll
+                                            for (int i = 0; i < 2; ++i) {
+                                                acc[u][4 * i] = fmaf(v[u][k][i].x, w, acc[u][4 * i]);
+                                                acc[u][4 * i + 1] = fmaf(v[u][k][i].y, w, acc[u][4 * i + 1]);
+                                                acc[u][4 * i + 2] = fmaf(v[u][k][i].z, w, acc[u][4 * i + 2]);
+                                                acc[u][4 * i + 3] = fmaf(v[u][k][i].w, w, acc[u][4 * i + 3]);
+                                            }
+                                        }
                                     }
                                 }
-                            }
 #pragma unroll
-                            for (int u = 0; u < 4; ++u) {
-                                const int e = e0 + u * kC_Softmax, er = e & (rows2 - 1), ec = e >> lrows;
-                                if (ec >= 16 || er >= n_rows) continue;
-                                const float inv = sh.joined[er].y;
-                                const long long o = ((long long)(now.row + (er >> a.log2g)) * a.Hkv + now.h << a.log2g) + (er & ((1 << a.log2g) - 1));
-                                uint4 w = make_uint4(0u, 0u, 0u, 0u);
-                                if (inv != 0.0f)
-                                    w = make_uint4(pack_bf16(acc[u][0] * inv, acc[u][1] * inv), pack_bf16(acc[u][2] * inv, acc[u][3] * inv),
-                                                   pack_bf16(acc[u][4] * inv, acc[u][5] * inv), pack_bf16(acc[u][6] * inv, acc[u][7] * inv));
-                                *reinterpret_cast<uint4 *>(a.out + o * kD + ec * 8) = w;
+                                for (int u = 0; u < kU; ++u) {
+                                    const int e = e0 + u * kC_Softmax, er = e & (rows2 - 1), ec = e >> lrows;
+                                    if (ec >= 16 || er >= n_rows) continue;
+                                    const float inv = sh.joined[er].y;
+                                    uint4 w = make_uint4(0u, 0u, 0u, 0u);
+                                    if (inv != 0.0f)
+                                        w = make_uint4(pack_bf16(acc[u][0] * inv, acc[u][1] * inv), pack_bf16(acc[u][2] * inv, acc[u][3] * inv),
+                                                       pack_bf16(acc[u][4] * inv, acc[u][5] * inv), pack_bf16(acc[u][6] * inv, acc[u][7] * inv));
+                                    *reinterpret_cast<uint4 *>(a.out + row_of(er) * kD + ec * 8) = w;
+                                }
                             }
-                        }
+                        };
+                        if (n_rows <= 32) join_parts(std::integral_constant<int, 1>{}, std::integral_constant<int, 8>{});
+                        else join_parts(std::integral_constant<int, 4>{}, std::integral_constant<int, 2>{});
                     }
                 }
                 if (settle) ok = join();
