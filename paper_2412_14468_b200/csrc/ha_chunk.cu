@@ -73,6 +73,7 @@ struct ChunkArgs {
 struct ChunkPart {
     int b, h, n, row, toks, first_pos, t0, t1;       // row: of q, the unit's first; toks: 0 behind the last part
     int split, cut, first_cta, n_parts;
+    int wild_v;                                      // a value that some row must not see is inf or NaN (see chunk_fetch)
 };
 // Four places: the keys of a part are asked for when all scores of the last but one have been ordered, so that no role is more than
 // three parts behind.
@@ -81,7 +82,7 @@ constexpr int kC_Parts = 4;
 struct ChunkShared {
     ChunkPart parts[kC_Parts];
     unsigned long long part_full[kC_Parts];
-    unsigned long long k_full[kC_SlotsK], k_empty[kC_SlotsK], v_full[kC_SlotsV], v_empty[kC_SlotsV], q_full, q_empty;
+    unsigned long long k_full[kC_SlotsK], k_empty[kC_SlotsK], v_full[kC_SlotsV], v_empty[kC_SlotsV], v_check[2], q_full, q_empty;
     unsigned long long s_full[2], s_free, p_full[2], o_done[2], joint, drained;
     long long start_rest;
     long long warp_sums[kC_Threads / 32];
@@ -152,12 +153,58 @@ __device__ __forceinline__ void chunk_fetch(const ChunkArgs &a, NextPart next_pa
     uint32_t phase = 1, issued = 0, issued_q = 0;     // phase of `empty`: the ring starts empty
     bool ok = true;
 
-    auto announce = [&]() {
+    // Of a tile with tokens that some rows must not see: weight 0 times inf or NaN is not 0, so such values become 0 here, and rows that do
+    // see them are given them back with the result.
+    bool check = false;                               // the pending tile is one
+    uint32_t part_now = 0, checks = 0, checks_issued = 0;
+    bool by_tma = false;                              // ... and lands at v_check, not by this warp's own copies
+    // an exponent of ones, and one more, carries into the sign's place
+    auto wild_bits = [](uint32_t w) -> uint32_t { return ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u; };
+    auto tame = [&]() {
+        const uint32_t at = ring + pending * kC_TileBytes + lane * 16;
+        uint32_t any = 0;
+#pragma unroll 1
+        for (int i0 = 0; i0 < kC_TileBytes / 512; i0 += 16) {
+            uint32_t w[16][4];
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[i][0]), "=r"(w[i][1]), "=r"(w[i][2]), "=r"(w[i][3]) : "r"(at + (i0 + i) * 512) : "memory");
+#pragma unroll
+            for (int i = 0; i < 16; ++i) any |= (wild_bits(w[i][0]) | wild_bits(w[i][1])) | (wild_bits(w[i][2]) | wild_bits(w[i][3]));
+        }
+        if (!__any_sync(0xffffffffu, any != 0)) return;
+#pragma unroll 1
+        for (int i = 0; i < kC_TileBytes / 128; ++i) {   // a word a lane
+            const uint32_t to = ring + pending * kC_TileBytes + i * 128 + lane * 4;
+            uint32_t w;
+            asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w) : "r"(to) : "memory");
+            if ((w & 0x7f80u) == 0x7f80u) w &= 0xffff0000u;
+            if ((w & 0x7f800000u) == 0x7f800000u) w &= 0x0000ffffu;
+            asm volatile("st.shared.b32 [%0], %1;" ::"r"(to), "r"(w) : "memory");
+        }
+        if (lane == 0) {
+            sh.parts[part_now % kC_Parts].wild_v = 1;
+            __threadfence_block();
+        }
+    };
+    // the pending tile, when all but the last kLeft groups of this warp's copies have landed
+    auto announce = [&](auto left) -> bool {
+        if (by_tma) {
+            if (!wait(sh.v_check[checks & 1u], checks >> 1 & 1u)) return false;
+            ++checks;
+        } else {
+            cp_async_wait<decltype(left)::value>();
+        }
+        __syncwarp();
+        if (kV && check) tame();
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&full[pending]));
         pending = -1;
+        return true;
     };
+    constexpr std::integral_constant<int, 0> kAll{};
+    constexpr std::integral_constant<int, 1> kButOne{};
     auto bad_page = [&](int page) -> bool {           // a page outside of the pool: zeros
         if ((unsigned)page < (unsigned)a.n_pages) return false;
         if (a.status) atomicOr(a.status, HA_DEV_BAD_INDEX);
@@ -203,27 +250,23 @@ __device__ __forceinline__ void chunk_fetch(const ChunkArgs &a, NextPart next_pa
         }
         cp_async_commit();
     };
-    auto load = [&](int j, bool by_threads) -> bool {
+    auto load = [&](int j, bool by_threads, bool wild) -> bool {
         if (by_threads) look_up(j);
         else {
             const int batch = (j * kChunkTile >> a.shift) >> 5;
             if (batch == ahead) fetch_pages(++ahead);
         }
         if (!mbar_test(smem_u32(&empty[slot]), phase)) {
-            if (pending >= 0) {                       // what is waited for may wait for these
-                cp_async_wait<0>();
-                announce();
-            }
+            if (pending >= 0 && !announce(kAll)) return false;   // what is waited for may wait for it
             if (!wait(empty[slot], phase)) return false;
         }
-        const uint32_t dst = ring + slot * kC_TileBytes, bar = smem_u32(&full[slot]);
+        const uint32_t dst = ring + slot * kC_TileBytes, bar = kV && wild && !by_threads ? smem_u32(&sh.v_check[checks_issued & 1u]) : smem_u32(&full[slot]);
         if (by_threads) {
             copy_rows(j, dst);
-            if (pending >= 0) {
-                cp_async_wait<1>();
-                announce();
-            }
+            if (pending >= 0 && !announce(kButOne)) return false;
             pending = slot;
+            check = wild;
+            by_tma = false;
         } else {
             // a lane for each box; boxes behind the end of the sequence are left out (their keys are masked, whatever they are)
             const int which = lane & ((1 << lboxes) - 1), half = lane >> lboxes, tok = j * kChunkTile + (which << lbox);
@@ -235,9 +278,11 @@ __device__ __forceinline__ void chunk_fetch(const ChunkArgs &a, NextPart next_pa
             if (which < there && half < (kV ? 1 : 2))
                 tma_load_rows(dst + ((uint32_t)which << lbox) * (kV ? 256 : 128) + (kV ? 0 : half * kC_Half), map, tok & mask, kV ? 0 : half, now.h, page, bar);
             ++issued;
-            if (pending >= 0) {
-                cp_async_wait<0>();
-                announce();
+            if (kV && wild) ++checks_issued;
+            if (pending >= 0 && !announce(kAll)) return false;
+            if (kV && wild) {
+                pending = slot;
+                check = by_tma = true;
             }
         }
         __syncwarp();
@@ -245,20 +290,20 @@ __device__ __forceinline__ void chunk_fetch(const ChunkArgs &a, NextPart next_pa
         return true;
     };
     for (uint32_t part = 0; ok && (ok = next_part(part, now)) && now.toks > 0; ++part) {
+        part_now = part;
         const int t0 = now.t0, t1 = now.t1;
         const bool tail = !kTma || (kV && (long long)t1 * kChunkTile > now.n);
+        // tiles from here on have tokens that the first of several new tokens must not see
+        const int hidden = kV && a.causal && now.toks > 1 ? (now.first_pos + 1 > 0 ? (now.first_pos + 1) >> 7 : 0) : 0x7fffffff;
         if (kTma) {
             ahead = (t0 * kChunkTile >> a.shift) >> 5;
             fetch_pages(ahead);
         }
         for (int j = t0; ok && j < t1; ++j) {
-            ok = load(j, !kTma || (tail && j == t1 - 1));
+            ok = load(j, !kTma || (tail && j == t1 - 1), j >= hidden);
             if (kV || !ok || j > t0) continue;
             // q, behind the first keys, which need not wait for its place
-            if (pending >= 0) {
-                cp_async_wait<0>();
-                announce();
-            }
+            if (pending >= 0 && !(ok = announce(kAll))) break;
             if (!(ok = part == 0 || wait(sh.q_empty, (part - 1) & 1u))) break;
             const int n_rows = now.toks << a.log2g, rows = n_rows <= kChunkTile ? kChunkTile : kChunkRows;
             if (kTma) {
@@ -286,9 +331,12 @@ __device__ __forceinline__ void chunk_fetch(const ChunkArgs &a, NextPart next_pa
             }
             __syncwarp();
         }
+        // before the next part is waited for: what the tile shows belongs to this one
+        if (ok && pending >= 0) ok = announce(kAll);
     }
     cp_async_wait<0>();
-    if (pending >= 0) announce();
+    if (!ok && kTma && kV)
+        for (; checks != checks_issued; ++checks) mbar_wait_parity(smem_u32(&sh.v_check[checks & 1u]), checks >> 1 & 1u);
     if (!ok && kTma) {   // never seen: what is in flight lands (one more bounded wait each) before shared memory is given up
         for (int i = 0; i < kSlots && i < (int)issued; ++i) {
             slot = slot == 0 ? kSlots - 1 : slot - 1;
@@ -317,6 +365,8 @@ __global__ void __launch_bounds__(kC_Threads, 1) chunk_attn_kernel(const __grid_
             mbar_init(smem_u32(&sh.v_full[i]), 1);
             mbar_init(smem_u32(&sh.v_empty[i]), 1);
         }
+        mbar_init(smem_u32(&sh.v_check[0]), 1);
+        mbar_init(smem_u32(&sh.v_check[1]), 1);
         mbar_init(smem_u32(&sh.q_full), 1);
         mbar_init(smem_u32(&sh.q_empty), 1);
         mbar_init(smem_u32(&sh.s_free), 4);
@@ -461,6 +511,7 @@ __global__ void __launch_bounds__(kC_Threads, 1) chunk_attn_kernel(const __grid_
                     now.row = walk.s.row0 + walk.unit.tok0; now.toks = walk.unit.toks; now.first_pos = walk.unit.first_pos;
                     now.t0 = walk.t0; now.t1 = walk.t1;
                     now.split = walk.unit.split; now.cut = walk.cut; now.first_cta = walk.first_cta; now.n_parts = walk.n_parts;
+                    now.wild_v = 0;
                 }
                 if (lane == 0) {
                     sh.parts[part % kC_Parts] = now;
@@ -709,6 +760,20 @@ __global__ void __launch_bounds__(kC_Threads, 1) chunk_attn_kernel(const __grid_
                             }
                         }
                         if (!mine) continue;
+                        if (now.wild_v) {              // what was taken out of the V tiles, for the tokens that this row sees
+                            const int first = now.first_pos + 1 > 0 ? (now.first_pos + 1) & ~(kChunkTile - 1) : 0, lo = t0 * kChunkTile;
+                            const int end = limit < t1 * kChunkTile ? limit : t1 * kChunkTile;
+                            for (int tok = first > lo ? first : lo; tok < end; ++tok) {
+                                const int page = a.table[(long long)now.b * a.bt_sb + (tok >> a.shift)];
+                                if ((unsigned)page >= (unsigned)a.n_pages) continue;
+                                const uint16_t *src = a.V.ptr + (long long)page * a.V.sb + (long long)now.h * a.V.sh + (long long)(tok & ((1 << a.shift) - 1)) * a.V.sn + c * 32;
+#pragma unroll
+                                for (int i = 0; i < 32; ++i) {
+                                    const uint32_t w = src[i];
+                                    if ((w & 0x7f80u) == 0x7f80u) v[i] = __float_as_uint(__uint_as_float(v[i]) + __uint_as_float(w << 16));
+                                }
+                            }
+                        }
                         if (now.cut) {
                             float4 *dst = reinterpret_cast<float4 *>(a.part_acc) + ((long long)slot * (kD / 4) + c * 8) * kChunkRows + r;
 #pragma unroll

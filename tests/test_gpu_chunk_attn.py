@@ -154,3 +154,143 @@ def test_sharp_scores_raise_the_maximum_often(ws):
 def test_single_token_split_over_the_whole_gpu(ws):
     go(ws, [50001], [1], Hkv=1, seed=9)
     go(ws, [30000, 9000], [1, 3], G=8, Hkv=8, seed=10)
+
+
+@pytest.mark.parametrize("page", [4, 16])
+@pytest.mark.parametrize("G", [1, 4])
+@pytest.mark.parametrize("m", [40, 300])
+def test_inf_and_nan_in_values_reach_only_the_rows_that_see_them(ws, G, m, page):
+    """Rows in front of the token are as if it had no such value (finite everywhere); rows that see it have it."""
+    n, Hkv = 700, 2
+    c = Case([n, 50], [m, 3], G=G, Hkv=Hkv, page=page, seed=m + G)
+    tok = {n - m + 7: float("nan"), n - m // 2: float("inf"), n - 1: float("-inf")}
+    before = Case([n, 50], [m, 3], G=G, Hkv=Hkv, page=page, seed=m + G)
+    before.run(ws)
+    for t, v in tok.items():
+        c.V[c.table[0, t // page].long(), 0, t % page, 5] = v
+    c.K[c.table[0, (n - 3) // page].long(), 1, (n - 3) % page, 9] = float("inf")       # a key that the rows in front must not see
+    c.run(ws)
+    torch.cuda.synchronize()
+    assert ha.ha_read_device_status(ws) == 0
+    got, clean = c.out.float(), before.out.float()
+    pos = torch.arange(n - m, n, device=DEV)
+    a, b = got[:m].view(m, Hkv, G, 128), clean[:m].view(m, Hkv, G, 128)
+    sees_nan, sees_inf = pos >= n - m + 7, pos >= n - m // 2
+    assert bool(torch.isnan(a[sees_nan, 0, :, 5]).all())
+    assert torch.equal(a[~sees_nan, 0], b[~sees_nan, 0])
+    keep = torch.arange(128, device=DEV) != 5
+    assert torch.equal(a[:, 0][..., keep], b[:, 0][..., keep])
+    assert torch.equal(a[pos < n - 3, 1], b[pos < n - 3, 1])                             # the other head: hidden key
+    assert torch.equal(got[m:], clean[m:])
+    assert int(sees_inf.sum()) > 0
+
+
+def test_inf_in_values_alone(ws):
+    c = Case([260], [130], G=2, Hkv=1, seed=21)
+    c.V[c.table[0, 200 // 16].long(), 0, 200 % 16, 3] = float("inf")
+    c.run(ws)
+    pos = torch.arange(130, 260, device=DEV)
+    assert bool((c.out[pos >= 200][:, :, 3] == float("inf")).all()) and bool(torch.isfinite(c.out[pos < 200]).all())
+
+
+def test_pages_that_do_not_exist_are_reported_and_other_sequences_are_right(ws):
+    for page in (2, 16, 128):
+        c = Case([500, 300, 40], [20, 1, 40], page=page, seed=22)
+        c.table[0, 3 if page < 128 else 1] = c.K.shape[0]
+        c.table[0, 0] = -1
+        c.run(ws)
+        torch.cuda.synchronize()
+        assert ha.ha_read_device_status(ws) == ha.HA_DEV_BAD_INDEX
+        ha.ha_workspace_init(ws)
+        c.k[0][:, :page] = 0
+        c.v[0][:, :page] = 0
+        at = (3 if page < 128 else 1) * page
+        c.k[0][:, at:at + page] = 0
+        c.v[0][:, at:at + page] = 0          # tokens on such pages read as zeros
+        c.check()
+
+
+@pytest.mark.parametrize("offsets", [[0, 50, 20], [-4, 3, 20], [0, 10, 21], [30, 40, 50]])
+def test_bad_offsets_leave_their_sequences_out(ws, offsets):
+    c = Case([100, 60], [10, 10], seed=23)
+    c.offsets = torch.tensor(offsets, dtype=torch.int32, device=DEV)
+    c.run(ws)
+    torch.cuda.synchronize()
+    assert ha.ha_read_device_status(ws) == ha.HA_DEV_BAD_INDEX
+    ha.ha_workspace_init(ws)
+    # a sequence is left out if its rows are not in ascending order or leave q; the others are computed
+    for b in range(2):
+        lo, hi = offsets[b], offsets[b + 1]
+        ok = 0 <= lo <= hi <= 20
+        if ok:
+            assert bool((c.out[lo:hi] != 7).any())
+    assert torch.isfinite(c.out.float()).all()
+
+
+def test_same_bits_again_and_on_another_stream(ws):
+    c = Case([9000, 300, 77], [150, 1, 77], G=8, Hkv=2, seed=24)
+    c.run(ws)
+    first = c.out.clone()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for _ in range(3):
+        c.out.fill_(7)
+        side.wait_stream(torch.cuda.current_stream())
+        c.run(ws, stream=side)
+        torch.cuda.current_stream().wait_stream(side)
+        assert torch.equal(c.out, first)
+    c.check(ws)
+
+
+def test_captured_and_replayed_with_other_lengths(ws):
+    """Two graphs share the workspace; lengths and rows are read when the graph runs."""
+    c, d = Case([3000, 1], [1, 1], seed=25), Case([700, 400], [90, 5], seed=26)
+    graphs = []
+    for x in (c, d):
+        x.run(ws)
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            x.run(ws)
+        graphs.append(g)
+    for _ in range(2):
+        for x, g in zip((c, d), graphs):
+            x.out.fill_(7)
+            g.replay()
+    torch.cuda.synchronize()
+    c.check(ws)
+    d.check(ws)
+    c.seq_lens.copy_(torch.tensor([2500, 1], dtype=torch.int32))
+    c.lens[0] = 2500
+    c.k[0], c.v[0] = c.k[0][:, :2500], c.v[0][:, :2500]
+    graphs[0].replay()
+    torch.cuda.synchronize()
+    c.check(ws)
+
+
+def test_results_do_not_need_32_byte_rows(ws):
+    c = Case([400, 33], [40, 33], seed=27)
+    whole = torch.empty(c.out.numel() + 8, dtype=torch.bfloat16, device=DEV)
+    c.out = whole[8:].view(c.out.shape)
+    c.out.fill_(7)
+    assert c.out.data_ptr() % 32 == 16
+    c.run(ws)
+    torch.cuda.synchronize()
+    c.check(ws)
+
+
+def test_a_cache_beyond_32_bit_offsets(ws):
+    """Pages at the far end of a pool of more than 2^32 bytes and 2^31 elements."""
+    page, Hkv = 64, 8
+    n_pages = 2 ** 31 // (Hkv * page * 128) + 40
+    K = torch.zeros(n_pages, Hkv, page, 128, dtype=torch.bfloat16, device=DEV)
+    c = Case([1000, 20], [30, 1], G=1, Hkv=Hkv, page=page, seed=28)
+    used = c.K.shape[0]
+    K[-used:] = c.K.nan_to_num(0)
+    V = torch.zeros_like(K)
+    V[-used:] = c.V.nan_to_num(0)
+    c.table[c.table >= 0] += n_pages - used
+    c.K, c.V = K, V
+    c.run(ws)
+    torch.cuda.synchronize()
+    c.check(ws)
