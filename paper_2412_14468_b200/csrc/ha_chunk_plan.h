@@ -21,15 +21,18 @@ constexpr int kChunkRows = 256;                    // query rows of a unit: two 
 constexpr int kChunkTile = 128;                    // tokens of a key tile
 // Cost of a key tile: two units for two row tiles; one where 128 rows or fewer let the two halves of a CTA take tiles in turn.
 constexpr int kChunkCostPair = 2, kChunkCostSplit = 1, kChunkCostMost = 2;
+// What a unit costs besides its tiles (its rows to fetch, results to write, the pipeline to fill: about 5 us, of pairs of tiles that take 1.9).
+constexpr int kChunkFixedPair = 8, kChunkFixedSplit = 2;
 
 struct ChunkSeq {   // one sequence
     int n, cnt, row0;                              // cached tokens, new ones among them, first row of q
     int units;                                     // per KV head
 };
 struct ChunkUnit {
-    int tok0, toks, tiles, cost;                   // first new token, new tokens, key tiles, cost of one
+    int tok0, toks, tiles, cost, fixed;            // first new token, new tokens, key tiles, cost of one, of the unit besides
     int first_pos;                                 // cache position of tok0 (< 0 where a sequence has more new tokens than cached ones)
     bool split;
+    HA_HD long long total() const { return (long long)tiles * cost + fixed; }
 };
 
 HA_HD int chunk_tokens_per_unit(int log2g) { return kChunkRows >> log2g; }
@@ -56,6 +59,7 @@ HA_HD ChunkUnit chunk_unit(const ChunkSeq &s, int u, int log2g, bool causal) {
     r.toks = s.cnt - r.tok0 < t ? s.cnt - r.tok0 : t;
     r.split = (r.toks << log2g) <= kChunkRows / 2;
     r.cost = r.split ? kChunkCostSplit : kChunkCostPair;
+    r.fixed = r.split ? kChunkFixedSplit : kChunkFixedPair;
     r.first_pos = s.n - s.cnt + r.tok0;
     r.tiles = chunk_tiles(causal ? (long long)r.first_pos + r.toks : (long long)s.n);
     return r;
@@ -75,7 +79,8 @@ HA_HD long long chunk_floor_sum(long long x, int lk) {
 // Cost of units 0 .. u - 1 of one KV head, all of them with all their tokens (u <= units, the last unit apart).
 HA_HD long long chunk_cost_full_units(const ChunkSeq &s, int u, int log2g, bool causal) {
     if (u <= 0) return 0;
-    if (!causal) return (long long)u * chunk_tiles(s.n) * kChunkCostPair;
+    const long long fixed = (long long)u * kChunkFixedPair;
+    if (!causal) return fixed + (long long)u * chunk_tiles(s.n) * kChunkCostPair;
     const int t = chunk_tokens_per_unit(log2g);
     const long long a = (long long)s.n - s.cnt;     // tokens in front of the new ones; negative: units that see nothing cost one tile
     long long m = u, skipped = 0;
@@ -87,7 +92,7 @@ HA_HD long long chunk_cost_full_units(const ChunkSeq &s, int u, int log2g, bool 
     const long long base = a + skipped * t + kChunkTile - 1;
     m -= skipped;
     long long tiles = skipped;
-    if (m == 0) return tiles * kChunkCostPair;
+    if (m == 0) return fixed + tiles * kChunkCostPair;
     if (t == 2 * kChunkTile) {
         // floor((base + 256 i) / 128) = floor(base / 128) + 2 i, base >= -255 + 127
         const long long q = base >> 7;              // rounds down
@@ -98,13 +103,13 @@ HA_HD long long chunk_cost_full_units(const ChunkSeq &s, int u, int log2g, bool 
         const long long q = base >> (8 - log2g);    // base > 127 - t >= -1
         tiles += chunk_floor_sum(q + m, lk) - chunk_floor_sum(q, lk);
     }
-    return tiles * kChunkCostPair;
+    return fixed + tiles * kChunkCostPair;
 }
 
 HA_HD long long chunk_cost_head(const ChunkSeq &s, int log2g, bool causal) {
     if (s.units == 0) return 0;
     const ChunkUnit last = chunk_unit(s, s.units - 1, log2g, causal);
-    return chunk_cost_full_units(s, s.units - 1, log2g, causal) + (long long)last.tiles * last.cost;
+    return chunk_cost_full_units(s, s.units - 1, log2g, causal) + last.total();
 }
 
 // CTAs that share W: every stretch is at least as long as the dearest tile, so that no part in the middle of a unit is empty.
@@ -114,11 +119,12 @@ HA_HD int chunk_ctas(long long W, int most) {
 }
 HA_HD long long chunk_bound(long long W, int C, int c) { return chunk_div(W * c, C); }
 HA_HD int chunk_cta_of(long long W, int C, long long x) { return (int)chunk_div((x + 1) * C - 1, W); }
-// first tile of a unit beginning at u0 that a stretch beginning at f takes
-HA_HD int chunk_first_tile(long long f, long long u0, int cost, int tiles) {
-    if (f <= u0) return 0;
-    const long long t = chunk_div(f - u0 + cost - 1, cost);
-    return t < tiles ? (int)t : tiles;
+// first tile of a unit beginning at u0 that a stretch beginning at f takes; the unit's fixed cost lies in front of its tiles
+HA_HD int chunk_first_tile(long long f, long long u0, const ChunkUnit &u) {
+    const long long g = f - u0 - u.fixed;
+    if (g <= 0) return 0;
+    const long long t = chunk_div(g + u.cost - 1, u.cost);
+    return t < u.tiles ? (int)t : u.tiles;
 }
 
 // The parts of a CTA's stretch in order.
@@ -156,12 +162,12 @@ struct ChunkWalk {
         u = lo;
         u0 = f0 - (rest - chunk_cost_full_units(s, u, log2g, causal));
         --u;
-        unit.tiles = unit.cost = 0;
+        unit.tiles = unit.cost = unit.fixed = 0;
     }
     // false: no part is left
     HA_HD bool next() {
         for (;;) {
-            u0 += (long long)unit.tiles * unit.cost;
+            u0 += unit.total();
             if (++u >= s.units) {
                 u = 0;
                 if (++h >= Hkv) {
@@ -174,15 +180,15 @@ struct ChunkWalk {
             }
             if (u0 >= f1) return false;
             unit = chunk_unit(s, u, log2g, causal);
-            t0 = chunk_first_tile(f0, u0, unit.cost, unit.tiles);
-            t1 = chunk_first_tile(f1, u0, unit.cost, unit.tiles);
+            t0 = chunk_first_tile(f0, u0, unit);
+            t1 = chunk_first_tile(f1, u0, unit);
             if (t0 < t1) break;
         }
         cut = t0 > 0 || t1 < unit.tiles;
         if (cut) {
-            first_cta = chunk_cta_of(W, C, u0);
-            int last = chunk_cta_of(W, C, u0 + (long long)unit.tiles * unit.cost - 1);
-            if (chunk_first_tile(chunk_bound(W, C, last), u0, unit.cost, unit.tiles) >= unit.tiles) --last;
+            first_cta = chunk_cta_of(W, C, u0 + unit.fixed);
+            int last = chunk_cta_of(W, C, u0 + unit.total() - 1);
+            if (chunk_first_tile(chunk_bound(W, C, last), u0, unit) >= unit.tiles) --last;
             n_parts = last - first_cta + 1;
         }
         return true;
