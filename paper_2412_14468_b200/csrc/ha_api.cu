@@ -589,12 +589,13 @@ int ha_chunk_attn_paged(const ha_shape *shape, const ha_tensor *q, const int32_t
                         const int32_t *seq_lens, int32_t causal, uint16_t *out, float *lse, void *workspace, size_t ws_bytes,
                         void *stream) {
     HA_TRY(check_shape(shape));
+    if (n_rows == 0) return HA_OK;   // an empty q need not have an address
     HA_TRY(check_rows(q));
     int shift;
     HA_TRY(check_paged_kv(K_pool, V_pool, n_pages, block_table, page_size, &shift));
     if (!q_offsets || !seq_lens || !out || n_rows < 0 || ((uintptr_t)out & 15)) return HA_ERR_INVALID_ARG;
     if (!workspace || ((uintptr_t)workspace & 255) || ws_bytes < chunk_workspace_bytes()) return HA_ERR_WORKSPACE;
-    if (shape->batch == 0 || n_rows == 0) return HA_OK;
+    if (shape->batch == 0) return HA_OK;
     HA_CUDA(launch_chunk_attn(shape->batch, shape->n_q_heads, shape->n_kv_heads, shape->sm_scale, view(q), q_offsets, n_rows,
                               view(K_pool), view(V_pool), n_pages, block_table, bt_stride_b, shift, seq_lens, causal != 0, out, lse,
                               workspace, (cudaStream_t)stream));
@@ -609,12 +610,12 @@ static int check_turn(const double *inv_freq, int32_t rot_dim, float scale) {
 
 int ha_rotary(const ha_tensor *x, const ha_tensor *y, int32_t n_rows, int32_t n_heads, const double *inv_freq, int32_t rot_dim,
               const int32_t *positions, int32_t interleaved, int32_t inverse, float scale, void *stream) {
+    HA_TRY(check_turn(inv_freq, rot_dim, scale));
+    if (n_rows == 0) return HA_OK;
     HA_TRY(check_rows(x));
     HA_TRY(check_rows(y));
-    HA_TRY(check_turn(inv_freq, rot_dim, scale));
     if (!positions || n_rows < 0 || n_heads <= 0) return HA_ERR_INVALID_ARG;
     if (n_heads > 65535) return HA_ERR_UNSUPPORTED;
-    if (n_rows == 0) return HA_OK;
     HA_CUDA(launch_rotary(view(x), view(y), n_rows, n_heads, inv_freq, rot_dim, positions, interleaved != 0, inverse != 0, scale,
                           (cudaStream_t)stream));
     return HA_OK;
@@ -660,6 +661,7 @@ int ha_rotary_append_paged(const ha_shape *shape, const ha_tensor *q, const ha_t
                            const ha_tensor *K_pool, const ha_tensor *V_pool, int32_t n_pages, const int32_t *block_table,
                            int64_t bt_stride_b, int32_t page_size, const int32_t *seq_lens, void *workspace, void *stream) {
     HA_TRY(check_shape(shape));
+    if (n_rows == 0) return HA_OK;
     HA_TRY(check_rows(q));
     HA_TRY(check_rows(k_new));
     HA_TRY(check_rows(v_new));
@@ -669,7 +671,7 @@ int ha_rotary_append_paged(const ha_shape *shape, const ha_tensor *q, const ha_t
     HA_TRY(check_paged_kv(K_pool, V_pool, n_pages, block_table, page_size, &shift));
     if (!q_offsets || !seq_lens || n_rows < 0 || ((uintptr_t)k_out & 15)) return HA_ERR_INVALID_ARG;
     if (workspace && ((uintptr_t)workspace & 255)) return HA_ERR_WORKSPACE;
-    if (shape->batch == 0 || n_rows == 0) return HA_OK;
+    if (shape->batch == 0) return HA_OK;
     HA_CUDA(launch_rotary_append(shape->batch, shape->n_q_heads, shape->n_kv_heads, view(q), view(k_new), view(v_new), view(q_out), k_out,
                                  q_offsets, n_rows, inv_freq, rot_dim, positions, interleaved != 0, scale, view(K_pool), view(V_pool),
                                  n_pages, block_table, bt_stride_b, shift, seq_lens, reinterpret_cast<uint32_t *>(workspace),

@@ -216,7 +216,7 @@ __device__ __forceinline__ void chunk_fetch(const ChunkArgs &a, NextPart next_pa
         const int e = batch * 32 + lane;
         int page = -1;
         if ((long long)e << a.shift < now.n) {
-            page = __ldg(a.table + (long long)now.b * a.bt_sb + e);
+            page = __ldcg(a.table + (long long)now.b * a.bt_sb + e);
             if (bad_page(page)) page = -1;
         }
         if (batch & 1) pages1 = page;
@@ -230,7 +230,7 @@ __device__ __forceinline__ void chunk_fetch(const ChunkArgs &a, NextPart next_pa
             const int tok = j * kChunkTile + g * 32 + lane;
             row_pages[g] = -1;
             if (tok < now.n) {
-                row_pages[g] = __ldg(a.table + (long long)now.b * a.bt_sb + (tok >> a.shift));
+                row_pages[g] = __ldcg(a.table + (long long)now.b * a.bt_sb + (tok >> a.shift));
                 if (bad_page(row_pages[g])) row_pages[g] = -1;
             }
         }
@@ -393,7 +393,7 @@ __global__ void __launch_bounds__(kC_Threads, 1) chunk_attn_kernel(const __grid_
     auto cost_of = [&](int b, bool report) -> long long {
         if (b >= a.B) return 0;
         bool bad;
-        const ChunkSeq s = chunk_seq(a.seq_lens[b], a.offsets[b], a.offsets[b + 1], a.n_rows, a.log2g, bad);
+        const ChunkSeq s = chunk_seq(HA_FROM_L2(a.seq_lens + b), HA_FROM_L2(a.offsets + b), HA_FROM_L2(a.offsets + b + 1), a.n_rows, a.log2g, bad);
         if (bad && report && a.status) atomicOr(a.status, HA_DEV_BAD_INDEX);
         return a.Hkv * chunk_cost_head(s, a.log2g, a.causal);
     };
@@ -764,12 +764,12 @@ __global__ void __launch_bounds__(kC_Threads, 1) chunk_attn_kernel(const __grid_
                             const int first = now.first_pos + 1 > 0 ? (now.first_pos + 1) & ~(kChunkTile - 1) : 0, lo = t0 * kChunkTile;
                             const int end = limit < t1 * kChunkTile ? limit : t1 * kChunkTile;
                             for (int tok = first > lo ? first : lo; tok < end; ++tok) {
-                                const int page = a.table[(long long)now.b * a.bt_sb + (tok >> a.shift)];
+                                const int page = __ldcg(a.table + (long long)now.b * a.bt_sb + (tok >> a.shift));
                                 if ((unsigned)page >= (unsigned)a.n_pages) continue;
                                 const uint16_t *src = a.V.ptr + (long long)page * a.V.sb + (long long)now.h * a.V.sh + (long long)(tok & ((1 << a.shift) - 1)) * a.V.sn + c * 32;
 #pragma unroll
                                 for (int i = 0; i < 32; ++i) {
-                                    const uint32_t w = src[i];
+                                    const uint32_t w = __ldcg(src + i);
                                     if ((w & 0x7f80u) == 0x7f80u) v[i] = __float_as_uint(__uint_as_float(v[i]) + __uint_as_float(w << 16));
                                 }
                             }

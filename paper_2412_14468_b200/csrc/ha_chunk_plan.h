@@ -14,6 +14,12 @@
 #else
 #define HA_HD inline
 #endif
+// Numbers that a kernel in front may have written after this one began: past L1, which may hold what was there before.
+#ifdef __CUDA_ARCH__
+#define HA_FROM_L2(p) __ldcg(p)
+#else
+#define HA_FROM_L2(p) (*(p))
+#endif
 
 namespace ha {
 
@@ -142,7 +148,7 @@ struct ChunkWalk {
 
     HA_HD void load() {
         bool bad;
-        s = chunk_seq(seq_lens[b], offsets[b], offsets[b + 1], n_rows, log2g, bad);
+        s = chunk_seq(HA_FROM_L2(seq_lens + b), HA_FROM_L2(offsets + b), HA_FROM_L2(offsets + b + 1), n_rows, log2g, bad);
     }
     // the unit that holds position f0, which lies `rest` behind the beginning of sequence b_
     HA_HD void begin(int cta, int b_, long long rest) {
@@ -163,6 +169,7 @@ struct ChunkWalk {
         u0 = f0 - (rest - chunk_cost_full_units(s, u, log2g, causal));
         --u;
         unit.tiles = unit.cost = unit.fixed = 0;
+        first_cta = n_parts = 0;
     }
     // false: no part is left
     HA_HD bool next() {

@@ -46,17 +46,17 @@ __device__ __forceinline__ void flag(uint32_t *status, uint32_t bit) { atomicOr(
 __global__ void __launch_bounds__(kP_Threads) pages_fork_kernel(const PageState p, const int32_t *__restrict__ parents,
                                                                const int32_t *__restrict__ children, int n) {
     pdl_wait();
-    const int i = blockIdx.x, parent = parents[i], child = children[i];
+    const int i = blockIdx.x, parent = __ldcg(parents + i), child = __ldcg(children + i);
     bool bad = parent < 0 || parent >= p.B || child < 0 || child >= p.B;
     for (int j = threadIdx.x; j < n; j += kP_Threads) {
-        const int c = children[j];
+        const int c = __ldcg(children + j);
         bad |= (c == child && j < i) || c == parent;   // a child twice: the first counts; no sequence is child and parent
     }
     int len = 0, pages = 0;
     if (!bad) {
-        len = p.seq_lens[parent];
+        len = __ldcg(p.seq_lens + parent);
         pages = pages_of(len > 0 ? len : 0, p.shift);
-        bad = p.seq_lens[child] != 0 || len < 0 || pages > p.width;
+        bad = __ldcg(p.seq_lens + child) != 0 || len < 0 || pages > p.width;
     }
     if (__syncthreads_or(bad)) {
         if (threadIdx.x == 0) flag(p.status, HA_DEV_BAD_INDEX);
@@ -65,7 +65,7 @@ __global__ void __launch_bounds__(kP_Threads) pages_fork_kernel(const PageState 
     const int32_t *from = p.table + (long long)parent * p.bt_sb;
     int32_t *to = p.table + (long long)child * p.bt_sb;
     for (int s = threadIdx.x; s < pages; s += kP_Threads) {
-        const int page = from[s];
+        const int page = __ldcg(from + s);
         to[s] = page;
         if ((unsigned)page < (unsigned)p.n_pages) atomicAdd(p.ref + page, 1);
         else flag(p.status, HA_DEV_BAD_INDEX);
@@ -76,22 +76,22 @@ __global__ void __launch_bounds__(kP_Threads) pages_fork_kernel(const PageState 
 // ---- free: every page of the sequence counts one holder less
 __global__ void __launch_bounds__(kP_Threads) pages_free_kernel(const PageState p, const int32_t *__restrict__ seqs, int n) {
     pdl_wait();
-    const int i = blockIdx.x, seq = seqs[i];
+    const int i = blockIdx.x, seq = __ldcg(seqs + i);
     if (seq < 0 || seq >= p.B) {
         if (threadIdx.x == 0) flag(p.status, HA_DEV_BAD_INDEX);
         return;
     }
     bool again = false;
-    for (int j = threadIdx.x; j < i; j += kP_Threads) again |= seqs[j] == seq;
+    for (int j = threadIdx.x; j < i; j += kP_Threads) again |= __ldcg(seqs + j) == seq;
     if (__syncthreads_or(again)) return;               // listed before
-    const int len = p.seq_lens[seq];
+    const int len = __ldcg(p.seq_lens + seq);
     int pages = pages_of(len > 0 ? len : 0, p.shift);
     if (pages > p.width) {
         if (threadIdx.x == 0) flag(p.status, HA_DEV_BAD_INDEX);
         pages = p.width;
     }
     for (int s = threadIdx.x; s < pages; s += kP_Threads) {
-        const int page = p.table[(long long)seq * p.bt_sb + s];
+        const int page = __ldcg(p.table + (long long)seq * p.bt_sb + s);
         bool ok = (unsigned)page < (unsigned)p.n_pages;
         if (ok && atomicSub(p.ref + page, 1) <= 0) {   // nobody holds it: the count goes back to what it was
             atomicAdd(p.ref + page, 1);
@@ -160,16 +160,16 @@ __global__ void __launch_bounds__(kP_Plan, 1) pages_plan_extend_kernel(const Pag
         int need = 0;
         bool copy = false;
         if (b < p.B) {
-            const int add = n_new[b], len = p.seq_lens[b];
+            const int add = __ldcg(n_new + b), len = __ldcg(p.seq_lens + b);
             if (add < 0 || len < 0) wrong |= HA_DEV_BAD_INDEX;
             else if (add > 0) {
                 const int have = pages_of(len, p.shift), want = pages_of((long long)len + add, p.shift);
                 if ((long long)len + add > 0x7fffffff || want > p.width) wrong |= HA_DEV_NO_PAGE;
                 else {
                     if (len & ((1 << p.shift) - 1)) {
-                        const int page = p.table[(long long)b * p.bt_sb + have - 1];
+                        const int page = __ldcg(p.table + (long long)b * p.bt_sb + have - 1);
                         if ((unsigned)page >= (unsigned)p.n_pages) wrong |= HA_DEV_BAD_INDEX;
-                        else copy = p.ref[page] > 1;
+                        else copy = __ldcg(p.ref + page) > 1;
                     }
                     need = want - have + (copy ? 1 : 0);
                 }
@@ -223,10 +223,10 @@ __global__ void __launch_bounds__(kP_Plan, 1) pages_plan_extend_kernel(const Pag
         }
         const int b = lo, f = plan.first[b];
         const bool copy = f < 0;
-        const int len = p.seq_lens[b], slot = pages_of(len, p.shift) - (copy ? 1 : 0) + r - (f & 0x7fffffff), page = plan.list[r];
+        const int len = __ldcg(p.seq_lens + b), slot = pages_of(len, p.shift) - (copy ? 1 : 0) + r - (f & 0x7fffffff), page = plan.list[r];
         int32_t *entry = p.table + (long long)b * p.bt_sb + slot;
         if (copy && r == (f & 0x7fffffff)) {
-            const int k = atomicAdd(&s_copies, 1), old = *entry;   // (the order of the list does not matter)
+            const int k = atomicAdd(&s_copies, 1), old = __ldcg(entry);   // (the order of the list does not matter)
             plan.src[k] = old;
             plan.dst[k] = page;
             atomicSub(p.ref + old, 1);
@@ -235,7 +235,7 @@ __global__ void __launch_bounds__(kP_Plan, 1) pages_plan_extend_kernel(const Pag
         p.ref[page] = 1;
     }
     __syncthreads();
-    for (int b = tid; b < p.B; b += kP_Plan) p.seq_lens[b] += n_new[b];
+    for (int b = tid; b < p.B; b += kP_Plan) p.seq_lens[b] = __ldcg(p.seq_lens + b) + __ldcg(n_new + b);
     if (tid == 0) plan.n_copies[0] = s_copies;
 }
 
@@ -306,10 +306,10 @@ __global__ void __launch_bounds__(kP_Copy) pages_copy_kernel(const PageState p, 
         const long long entries = (long long)p.B * p.width;
         for (long long e = at; e < entries; e += stride) {
             const int b = (int)(e / p.width), s = (int)(e % p.width);
-            const int len = p.seq_lens[b];
-            int page = t.table[(long long)b * p.bt_sb + s];
+            const int len = __ldcg(p.seq_lens + b);
+            int page = __ldcg(t.table + (long long)b * p.bt_sb + s);
             if (s < pages_of(len > 0 ? len : 0, p.shift)) {
-                if ((unsigned)page < (unsigned)p.n_pages) page = t.page_map[page];
+                if ((unsigned)page < (unsigned)p.n_pages) page = __ldcg(t.page_map + page);
                 else flag(p.status, HA_DEV_BAD_INDEX);
             }
             t.table_out[(long long)b * t.out_sb + s] = page;
@@ -317,12 +317,12 @@ __global__ void __launch_bounds__(kP_Copy) pages_copy_kernel(const PageState p, 
         // counts: a moved page's goes with it and leaves 0; every count is read and written by one thread
         const int U = n + plan.n_copies[1];
         for (long long e = at; e < p.n_pages; e += stride) {
-            const bool stays = t.page_map[e] == (int)e;
-            if (stays) t.ref_out[e] = t.ref[e];
-            else if (e >= U && t.page_map[e] < 0) t.ref_out[e] = 0;
+            const int to = __ldcg(t.page_map + e);
+            if (to == (int)e) t.ref_out[e] = __ldcg(t.ref + e);
+            else if (e >= U && to < 0) t.ref_out[e] = 0;
         }
         for (long long m = at; m < n; m += stride) {
-            const int v = t.ref[src[m]];
+            const int v = __ldcg(t.ref + src[m]);
             t.ref_out[src[m]] = 0;
             t.ref_out[dst[m]] = v;
         }

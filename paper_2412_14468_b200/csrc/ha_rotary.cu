@@ -10,6 +10,7 @@
 // rounding is p w 2^-53.  The top bits become a float for sincospif.
 //
 // What bounds it: HBM (a row of 256 bytes is read and written once), and for a few tokens the launch and two dependent loads.
+// All loads go past L1, which may hold what was there before a kernel in front wrote (see the note on programmatic launches).
 // Eight lanes hold the cosines and sines of a token (eight pairs each, once for all its heads) and take its heads one after the
 // other, 16 values at a time; the four such groups of a warp take every fourth head.
 #include "ha_common.cuh"
@@ -57,7 +58,7 @@ __device__ __forceinline__ void rotary_angles(const RotaryTurn &t, int first, in
     if (first >= t.half) return;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        double f = __ldg(t.inv_freq + first + i) * 0.15915494309189533577;   // turns per position
+        double f = __ldcg(t.inv_freq + first + i) * 0.15915494309189533577;   // turns per position
         f -= floor(f);
         const unsigned long long turn = (unsigned long long)(long long)p * __double2ull_rn(f * 18446744073709551616.0);
         const float half_turns = __ll2float_rn((long long)turn) * 1.0842021724855044e-19f;   // 2^-63: in [-1, 1]
@@ -110,7 +111,7 @@ __device__ __forceinline__ int sequence_of(const int32_t *offsets, int B, int ro
     int lo = 0, n = B + 1;                // offsets[lo .. lo + n) are left, all in front of lo are <= row
     for (;;) {
         const int step = (n + 31) / 32, i = lo + lane * step;
-        const bool le = lane * step < n && __ldg(offsets + i) <= row;
+        const bool le = lane * step < n && __ldcg(offsets + i) <= row;
         const uint32_t m = __ballot_sync(0xffffffffu, le);
         if (m == 0) return -1;            // only in the first round: row lies in front of the first
         const int at = 31 - __clz(m);
@@ -135,15 +136,15 @@ __global__ void __launch_bounds__(kR_Threads) rotary_kernel(const RotaryArgs a) 
     if (kAppend) {
         const int b = sequence_of(a.offsets, a.B, row, lane);
         if (b < 0) return;
-        const int o0 = __ldg(a.offsets + b), o1 = __ldg(a.offsets + b + 1);
+        const int o0 = __ldcg(a.offsets + b), o1 = __ldcg(a.offsets + b + 1);
         if (o0 < 0 || o1 > a.rows || row >= o1) {   // rows of no sequence; offsets that are not ascending or leave the rows
             if (a.status && (o0 < 0 || o1 > a.rows || o1 < o0) && lane == 0) atomicOr(a.status, HA_DEV_BAD_INDEX);
             return;
         }
-        const int tok = __ldg(a.seq_lens + b) - o1 + row;
-        pos = a.positions ? __ldg(a.positions + row) : tok;
+        const int tok = __ldcg(a.seq_lens + b) - o1 + row;
+        pos = a.positions ? __ldcg(a.positions + row) : tok;
         if (tok >= 0) {
-            const int page = __ldg(a.table + (long long)b * a.bt_sb + (tok >> a.shift));
+            const int page = __ldcg(a.table + (long long)b * a.bt_sb + (tok >> a.shift));
             if ((unsigned)page < (unsigned)a.n_pages) {
                 const long long slot = tok & ((1 << a.shift) - 1);
                 k_at = (long long)page * a.K.sb + slot * a.K.sn;
@@ -151,7 +152,7 @@ __global__ void __launch_bounds__(kR_Threads) rotary_kernel(const RotaryArgs a) 
             } else if (a.status && lane == 0) atomicOr(a.status, HA_DEV_BAD_INDEX);
         }
     } else {
-        pos = __ldg(a.positions + row);
+        pos = __ldcg(a.positions + row);
     }
 
     const int turned = a.turn.half / 8;
@@ -180,7 +181,7 @@ __global__ void __launch_bounds__(kR_Threads) rotary_kernel(const RotaryArgs a) 
             dst = v_at < 0 ? nullptr : const_cast<uint16_t *>(a.V.ptr) + v_at + (long long)g * a.V.sh;
             turn = false;
         }
-        uint4 va = *reinterpret_cast<const uint4 *>(src + pa), vb = *reinterpret_cast<const uint4 *>(src + pb);
+        uint4 va = __ldcg(reinterpret_cast<const uint4 *>(src + pa)), vb = __ldcg(reinterpret_cast<const uint4 *>(src + pb));
         rotary_apply(a.turn, turn, c, s, va, vb);
         if (dst) {
             *reinterpret_cast<uint4 *>(dst + pa) = va;
