@@ -399,7 +399,8 @@ int ha_chunk_attn_paged(const ha_shape *shape, const ha_tensor *q, const int32_t
  * integers, so far positions lose nothing; sines, cosines and products are fp32, one rounding to bf16.
  *   x, y         bf16 rows [n_rows][n_heads][128]: stride_n steps over rows, stride_h over heads (stride_b is not used), multiples
  *                of 8; y may be x (in place), else they must not overlap
- *   inv_freq     f64 [rot_dim / 2], radians per position (device), e.g. from ha_rotary_freqs
+ *   inv_freq     f64 [rot_dim / 2], radians per position (device), e.g. from ha_rotary_freqs; like a mapping network it must not be
+ *                written by a kernel in front that releases its dependents early
  *   rot_dim      multiple of 16, 16 .. 128
  *   positions    i32 [n_rows] (device), any value */
 int ha_rotary(const ha_tensor *x, const ha_tensor *y, int32_t n_rows, int32_t n_heads, const double *inv_freq, int32_t rot_dim,

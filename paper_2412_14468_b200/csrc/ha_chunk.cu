@@ -24,6 +24,10 @@
 // and 0.85 us for a V tile in one.  By threads: the V tile that a sequence ends in, as rows behind the end have to be
 // zeros (0 times what lies there need not be 0); and everything where pages have fewer than 8 tokens (the swizzle repeats every
 // 8 rows) or no tensor map takes the strides.
+// What bounds it: a pair of tiles (256 rows x 128 keys) is 2048 cycles of MMAs and 2048 of exponentials, and takes about 3000: a row
+// tile's softmax is one chain (scores to registers 100 cycles, maximum 400, vote 110, exponentials 1400, weights and barriers 300).
+// Measured: 2048 new tokens of 16384, 32 heads, pages of 16: 411 us, 1250 TFLOP/s (0.75 of a large bf16 product); 32 sequences of
+// 16384 with one new token: 333 us, 6.4 TB/s; one of 4096: 17 us, a chain of latencies.
 // A unit cut between CTAs: each part writes m, l and O to the workspace; the part that arrives last joins them all, in the order of
 // the keys, so that results do not depend on the order of arrival.
 // Every wait is bounded: a waiter that gives up raises HA_DEV_TIMEOUT, all roles stop, the MMAs in flight are waited for and the

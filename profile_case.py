@@ -49,6 +49,31 @@ def prefill(args):
     print("key bytes per call:", B * Hkv * T * 256, " algorithmic flop per call:", B * Hkv * T * 2 * (128 * 128 * 2 + 128 * 32))
 
 
+def chunk(args):
+    """ha_chunk_attn_paged: --batch sequences of --chunk's first number of cached tokens, its second of them new, pages of its third."""
+    n, m, page = args.chunk
+    B, Hkv, G, dev = args.batch or 1, 8, 4, "cuda:0"
+    torch.cuda.set_device(0)
+    g = torch.Generator(dev).manual_seed(wl.BASE_SEED + 79)
+    pages = -(-n // page)
+    K, V = (torch.randn(B * pages, Hkv, page, 128, device=dev, generator=g).to(torch.bfloat16) for _ in range(2))
+    table = torch.randperm(B * pages, device=dev, generator=g).to(torch.int32).view(B, pages)
+    q = (2 * torch.randn(B * m, G * Hkv, 128, device=dev, generator=g)).to(torch.bfloat16)
+    offsets = torch.arange(0, B * m + 1, m, dtype=torch.int32, device=dev)
+    lens = torch.full((B,), n, dtype=torch.int32, device=dev)
+    out, ws = torch.empty_like(q), ha.alloc_workspace_chunk(device=dev)
+    shape = ha.make_shape(B, G * Hkv, Hkv, 128 ** -0.5)
+    pairs = B * (m * n - m * (m - 1) // 2) * G * Hkv
+    for s in range(args.steps):
+        e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        e0.record()
+        ha.ha_chunk_attn_paged(shape, q, offsets, K, V, table, page, lens, out, ws)
+        e1.record()
+        torch.cuda.synchronize()
+        us = e0.elapsed_time(e1) * 1e3
+        print(f"step {s}: {us:.1f} us, {512 * pairs / us / 1e6:.0f} TFLOP/s, {B * n * Hkv * 512 / us / 1e3:.0f} GB/s of keys and values")
+
+
 def score_only(args):
     cfg = wl.CONFIGS[args.config]
     B = args.batch if args.batch is not None else cfg.batch
@@ -210,6 +235,8 @@ def main():
     ap.add_argument("--score-topk-wide", action="store_true",
                     help="SCORE + TOPK on signatures of 64 and 512 bits (ha_score_topk_wide) on --tokens tokens")
     ap.add_argument("--encode-only", action="store_true", help="ENCODE of one decode step alone (--batch sequences)")
+    ap.add_argument("--chunk", type=int, nargs=3, metavar=("CACHED", "NEW", "PAGE"), default=None,
+                    help="attention of new tokens over pages alone (--batch sequences, 32 query and 8 KV heads)")
     ap.add_argument("--pipelined", action="store_true",
                     help="run the step through ha_sparse_decode_pipelined (SCORE + TOPK ahead of GATHER-ATT in one persistent kernel)")
     ap.add_argument("--tokens", type=int, default=1 << 23)
@@ -222,6 +249,8 @@ def main():
         return encode_only(args)
     if args.score_only:
         return score_only(args)
+    if args.chunk:
+        return chunk(args)
     if args.prefill:
         return prefill(args)
     cfg = wl.CONFIGS[args.config]
