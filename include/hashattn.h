@@ -381,7 +381,7 @@ int ha_sparse_decode_paged_codes(const ha_shape *shape, const ha_mapping *map_q,
  *   K_pool, V_pool, block_table, page_size   as in ha_gather_attn_paged, except that the two pools' strides need not agree; n_pages
  *                bounds the page numbers: tokens on a page outside 0 .. n_pages - 1 read as zeros and raise HA_DEV_BAD_INDEX (the
  *                sequence's output is then of no use)
- *   out          bf16 [n_rows][n_q_heads][128] contiguous; lse fp32 [n_rows][n_q_heads] or NULL
+ *   out          bf16 [n_rows][n_q_heads][128] contiguous, apart from q; lse fp32 [n_rows][n_q_heads] or NULL
  *   workspace    ha_workspace_bytes_chunk() bytes, the same for all shapes; prepared once with ha_workspace_init
  * n_sink / n_local of the shape are not looked at.  Results do not depend on how the work is split: the same call gives the same
  * bits.  If a wait inside the kernel runs out (it never should) it raises HA_DEV_TIMEOUT and out must not be used; call

@@ -79,9 +79,10 @@ struct ChunkPart {
     int split, cut, first_cta, n_parts;
     int wild_v;                                      // a value that some row must not see is inf or NaN (see chunk_fetch)
 };
-// Four places: the keys of a part are asked for when all scores of the last but one have been ordered, so that no role is more than
-// three parts behind.
-constexpr int kC_Parts = 4;
+// Part p is written when all scores of part p - 2 have been ordered.  Then row tile 0 has the scores of p - 3 and is done with p - 4, but row
+// tile 1, which has nothing to do in a part of one key tile, may still be writing the results of p - 4 (it has to join in p - 3 before
+// row tile 0 goes on to p - 2).  So five places are needed at least.
+constexpr int kC_Parts = 8;
 
 struct ChunkShared {
     ChunkPart parts[kC_Parts];

@@ -294,3 +294,44 @@ def test_a_cache_beyond_32_bit_offsets(ws):
     c.run(ws)
     torch.cuda.synchronize()
     c.check(ws)
+
+
+@pytest.mark.parametrize("G", [1, 8])
+def test_short_sequences_right_behind_a_prompt(ws, G):
+    """A CTA goes from units of two row tiles to many of one key tile each, which only one of its halves works on."""
+    lens, new = [], []
+    for i in range(40):
+        lens += [700 + i] + [3 + i] * 12
+        new += [300 + i] + [1] * 12
+    c = Case(lens, new, G=G, Hkv=1, seed=30)
+    c.run(ws)
+    torch.cuda.synchronize()
+    c.check(ws)
+    first = c.out.clone()
+    for _ in range(30):
+        c.out.fill_(7)
+        c.run(ws)
+        assert torch.equal(c.out, first)
+
+
+def test_two_calls_at_once(ws):
+    """Streams of their own, workspaces of their own."""
+    other = ha.alloc_workspace_chunk()
+    c, d = Case([5000, 40], [64, 1], seed=31), Case([900] * 20, [1] * 20, seed=32)
+    torch.cuda.synchronize()
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+    for _ in range(5):
+        c.run(ws, stream=a)
+        d.run(other, stream=b)
+    torch.cuda.synchronize()
+    c.check(ws)
+    d.check(other)
+
+
+def test_no_rows_and_no_sequences(ws):
+    c = Case([100], [0], seed=33)
+    c.run(ws)
+    q = torch.empty(0, 8, 128, dtype=torch.bfloat16, device=DEV)
+    ha.ha_chunk_attn_paged(c.shape, q, torch.zeros(2, dtype=torch.int32, device=DEV), c.K, c.V, c.table, c.page, c.seq_lens, torch.empty_like(q), ws)
+    torch.cuda.synchronize()
+    assert ha.ha_read_device_status(ws) == 0

@@ -261,3 +261,27 @@ def test_extend_looks_through_the_whole_pool():
     assert c.extend([0, 1]) == ha.HA_DEV_NO_PAGE
     c.do_extend([0, 1])
     c.check(ha.HA_DEV_NO_PAGE)
+
+
+def test_fork_extend_and_free_captured_once_and_replayed():
+    """A graph whose replays go on from the state that the last one left."""
+    c = Cache(9, 30, 120, 4, seed=9)
+    c.extend([30] + [0] * 8)
+    c.do_extend([30] + [0] * 8)
+    parents, kids, add, gone = c.ints([0] * 4), c.ints([1, 2, 3, 4]), c.ints([3, 2, 1, 0, 5] + [0] * 4), c.ints([4, 1, 3, 2])
+
+    def step():
+        ha.ha_pages_fork(parents, kids, c.d_lens, c.d_table, c.page, c.d_ref, c.ws)
+        ha.ha_pages_extend(add, c.d_lens, c.d_table, c.page, c.d_ref, c.K, c.V, c.codes, c.ws)
+        ha.ha_pages_free(gone, c.d_lens, c.d_table, c.page, c.d_ref, c.ws)
+
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        step()
+    for _ in range(20):
+        g.replay()
+        flag = c.fork([0] * 4, [1, 2, 3, 4]) | c.extend([3, 2, 1, 0, 5] + [0] * 4) | c.free([4, 1, 3, 2])
+        if flag:
+            break
+    torch.cuda.synchronize()
+    c.check(flag)
