@@ -6,7 +6,7 @@
 // One pass over the keys with a running maximum m and sum l per row: p = 2^(s - m) in 32 bits, l += p, O += bf16(p) V; the maximum
 // that the exponents refer to is raised, and O and l rescaled, only when a tile's maximum lies more than 2^8 above it, so that most
 // tiles leave O alone (p <= 2^8: sums stay far inside 32 bits).  p is rounded to bf16 for the tensor cores, as V is bf16 and both
-// operands have one type: half a step, 2^-9 relative, on each weight, of independent sign; l sums the unrounded p.
+// operands have one type: at most half a step, 2^-8 relative, on each weight, of independent sign; l sums the unrounded p.
 //
 // Work: see ha_chunk_plan.h.  A CTA holds two tiles of 128 query rows (tokens x heads of a group, so that one fetch of K and V
 // serves the whole group) and streams key tiles of 128 tokens through two rings in shared memory.
@@ -19,9 +19,9 @@
 // the last one, and neither waits for the other.  (With an S of its own for each row tile, overwritten by P, a tile's two
 // products and its softmax formed one chain of 3700 cycles, 2048 of them with the tensor cores at work.)
 // A unit of at most 128 rows (a decoding sequence) uses the two halves for alternate key tiles and joins them at its end.
-// Fetching: by TMA, a box for the rows of one page (or 128 of them).  A box costs 45 ns and 1.3 ns a row however it is issued (measured), so pages of 16
-// take 1.0 us for a K tile in two boxes a page (one for either half of the columns, which a K-major operand of 128 rows needs)
-// and 0.85 us for a V tile in one.  By threads: the V tile that a sequence ends in, as rows behind the end have to be
+// Fetching: by TMA, a box for the rows of one page (or 128 of them).  A box costs 45 ns and 1.3 ns a row of an issuing thread's time
+// however it is issued (measured), so pages of 16 take 1.0 us for a K tile in two boxes a page (one for either half of the columns,
+// which a K-major operand of 128 rows needs) and 0.85 us for a V tile in one.  By threads: the V tile that a sequence ends in, as rows behind the end have to be
 // zeros (0 times what lies there need not be 0); and everything where pages have fewer than 8 tokens (the swizzle repeats every
 // 8 rows) or no tensor map takes the strides.
 // What bounds it: a pair of tiles (256 rows x 128 keys) is 2048 cycles of MMAs and 2048 of exponentials, and takes about 3000: a row
@@ -30,8 +30,8 @@
 // 16384 with one new token: 333 us, 6.4 TB/s; one of 4096: 17 us, a chain of latencies.
 // A unit cut between CTAs: each part writes m, l and O to the workspace; the part that arrives last joins them all, in the order of
 // the keys, so that results do not depend on the order of arrival.
-// Every wait is bounded: a waiter that gives up raises HA_DEV_TIMEOUT, all roles stop, the MMAs in flight are waited for and the
-// tensor memory is given back.
+// Every wait is bounded: a waiter that gives up raises HA_DEV_TIMEOUT and stops, those that wait for it run out as well, and the MMAs
+// and copies in flight are waited for before the tensor memory is given back.
 #include "ha_attn_dev.cuh"
 #include "ha_chunk_plan.h"
 #include "ha_encode_dev.cuh"
@@ -94,7 +94,6 @@ struct ChunkShared {
     int start_b;
     int last_part;
     uint32_t tmem;
-    volatile int fail;
     union {
         float ml[2][128][2];     // the halves' maxima and sums, where they share a unit
         float2 joined[kChunkRows];   // of the rows of a unit whose parts are joined: maximum, one over the sum
@@ -383,7 +382,6 @@ __global__ void __launch_bounds__(kC_Threads, 1) chunk_attn_kernel(const __grid_
         mbar_init(smem_u32(&sh.joint), kC_Softmax / 32);
         mbar_init(smem_u32(&sh.drained), 2);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        sh.fail = 0;
         sh.start_b = -1;
     }
     pdl_wait();
@@ -479,20 +477,20 @@ __global__ void __launch_bounds__(kC_Threads, 1) chunk_attn_kernel(const __grid_
     tc_fence_after();
     const uint32_t tmem = sh.tmem;
 
+    // (the answer goes by the barrier alone, so that the lanes of a warp get the same one; the roles behind one that gave up run out too)
     auto gave_up = [&]() -> bool {
-        sh.fail = 1;
         if (a.status) atomicOr(a.status, HA_DEV_TIMEOUT);
         return false;
     };
     auto wait = [&](unsigned long long &bar, uint32_t parity) -> bool {
         const uint32_t at = smem_u32(&bar);
         if (mbar_test(at, parity)) return true;
-        return mbar_wait_parity(at, parity) ? sh.fail == 0 : gave_up();
+        return mbar_wait_parity(at, parity) || gave_up();
     };
     auto wait_parked = [&](unsigned long long &bar, uint32_t parity) -> bool {   // where nobody waits for the waiter
         const uint32_t at = smem_u32(&bar);
         if (mbar_test(at, parity)) return true;
-        return mbar_wait_parity<0>(at, parity) ? sh.fail == 0 : gave_up();
+        return mbar_wait_parity<0>(at, parity) || gave_up();
     };
 
     if (warp >= kC_WarpS) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kC_RegsOther));
