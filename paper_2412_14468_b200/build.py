@@ -35,7 +35,7 @@ def sources():
 
 
 def _headers():
-    return glob.glob(os.path.join(CSRC, "*.cuh")) + glob.glob(os.path.join(ROOT, "include", "*.h"))
+    return [p for d, ends in ((CSRC, "*.cuh"), (CSRC, "*.h"), (os.path.join(ROOT, "include"), "*.h")) for p in glob.glob(os.path.join(d, ends))]
 
 
 def _obj(src: str) -> str:
