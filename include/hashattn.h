@@ -16,9 +16,10 @@
  *     default stream).
  *   - Calls only enqueue work on `stream`: no host synchronisation and no allocation, except
  *     where stated (ha_read_device_status, ha_sparse_decode_host, ha_sparse_decode_paged_host).
- *   - Scratch memory is one caller-owned workspace of at least ha_workspace_bytes(...) bytes,
- *     256-byte aligned, prepared once with ha_workspace_init.  Calls that share a workspace must
- *     be ordered on one stream.
+ *   - Scratch memory is one caller-owned workspace of at least ha_workspace_bytes(...) bytes (or the
+ *     ha_workspace_bytes_*(...) that a call names), 256-byte aligned, prepared once with
+ *     ha_workspace_init.  Calls of every kind and shape may share one that is large enough for each of
+ *     them; they must be ordered on one stream.
  *   - Kernels are launched with programmatic stream serialization: a kernel may start while its
  *     predecessor in the stream is finishing, and before it waits for that predecessor it reads the
  *     mapping networks, seq_lens, k_per_seq and key signatures that lie in a contiguous 32-bit cache
@@ -109,13 +110,14 @@ typedef struct ha_tensor {
     int64_t stride_n;
 } ha_tensor;
 
-/* Bytes of workspace needed by every entry point for shapes up to (shape, max_seq_len, max_k).
+/* Bytes of workspace needed by every entry point for shapes up to (shape, max_seq_len, max_k), those apart that name a
+ * ha_workspace_bytes_*(...) of their own.
  * Returns 0 if the shape is unsupported.  The size depends on the batch, the head counts and
  * max_seq_len; max_k (>= 0) is checked but does not enter the size, because index lists are the
  * caller's own buffers. */
 size_t ha_workspace_bytes(const ha_shape *shape, int32_t max_seq_len, int32_t max_k);
 
-/* Clears the workspace header (device status word).  Call once after allocating the workspace
+/* Clears the workspace's header (device status word) and its counters.  Call once after allocating the workspace
  * and whenever the status should be reset. */
 int ha_workspace_init(void *workspace, size_t ws_bytes, void *stream);
 

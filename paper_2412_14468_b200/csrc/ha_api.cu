@@ -81,10 +81,8 @@ size_t ha_workspace_bytes(const ha_shape *shape, int32_t max_seq_len, int32_t ma
 
 int ha_workspace_init(void *workspace, size_t ws_bytes, void *stream) {
     if (!workspace || ((uintptr_t)workspace & 255) || ws_bytes < kHeaderBytes) return HA_ERR_WORKSPACE;
-    // status and abort words, the ticket counters and the release counters (which every call leaves at zero again)
-    size_t n = kHeaderBytes + (size_t)3 * kMaxUnits * 4;
-    if (n > ws_bytes) n = ws_bytes;
-    HA_CUDA(cudaMemsetAsync(workspace, 0, n, (cudaStream_t)stream));
+    // status and abort words, and the counters (which every call leaves at zero again)
+    HA_CUDA(cudaMemsetAsync(workspace, 0, ws_bytes < kWorkspaceFront ? ws_bytes : kWorkspaceFront, (cudaStream_t)stream));
     return HA_OK;
 }
 

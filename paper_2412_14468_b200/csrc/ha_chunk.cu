@@ -938,9 +938,9 @@ __global__ void __launch_bounds__(kC_Threads, 1) chunk_attn_kernel(const __grid_
     }
 }
 
-// ---- workspace: header, tickets, parts
+// ---- workspace: front (the tickets in it), parts
 size_t chunk_workspace_bytes() {
-    return kHeaderBytes + kChunkMaxCtas * 4 + (size_t)2 * kChunkMaxCtas * kChunkRows * (2 + kD) * 4;
+    return kWorkspaceFront + (size_t)2 * kChunkMaxCtas * kChunkRows * (2 + kD) * 4;
 }
 
 // Tensor maps (bf16, strides in elements): q [n_rows][Hq][128] and a pool [n_pages][Hkv][page][128], both with the 128 columns as two
@@ -996,8 +996,8 @@ cudaError_t launch_chunk_attn(int B, int Hq, int Hkv, float sm_scale, TensorView
     a.out = out; a.lse = lse;
     char *ws = reinterpret_cast<char *>(workspace);
     a.status = reinterpret_cast<uint32_t *>(ws);
-    a.tickets = reinterpret_cast<int32_t *>(ws + kHeaderBytes);
-    a.part_ml = reinterpret_cast<float *>(ws + kHeaderBytes + kChunkMaxCtas * 4);
+    a.tickets = reinterpret_cast<int32_t *>(ws + kOffChunkTickets);
+    a.part_ml = reinterpret_cast<float *>(ws + kWorkspaceFront);
     a.part_acc = a.part_ml + (size_t)2 * kChunkMaxCtas * kChunkRows * 2;
     CUtensorMap mq, mk, mv;
     memset(&mq, 0, sizeof(mq));

@@ -19,7 +19,17 @@ constexpr int kMaxBalancedUnits = 1024;   // above this many (sequence, KV head)
 constexpr int kMaxGroup = 8;        // query heads per KV head
 constexpr size_t kHeaderBytes = 256;   // device status word (+ padding)
 constexpr int kChunkMaxCtas = 160;       // CTAs of the attention of new tokens (bounds its tickets and parts)
-constexpr int kMaxUnits = 65536;       // (sequence, KV head) pairs: bounds the ticket region
+constexpr int kMaxUnits = 65536;       // (sequence, KV head) pairs
+
+// Workspaces.  A caller may give one workspace to calls of every kind and shape, one after the other, so every layout begins alike:
+// the header, then all counters that calls of one kind find at zero and leave at zero, whichever the kind; what any call leaves
+// behind otherwise lies further on.  ha_workspace_init clears that front.
+//   header     word 0: device status, 1 .. 7: the pipelined step
+//   counters   i32 [3][units] of the decode step, units <= kMaxBalancedUnits: with more, no unit is cut and none is counted
+//   tickets    i32 [kChunkMaxCtas] of the attention of new tokens
+constexpr size_t kOffCounters = kHeaderBytes;
+constexpr size_t kOffChunkTickets = kOffCounters + (size_t)3 * kMaxBalancedUnits * 4;
+constexpr size_t kWorkspaceFront = (kOffChunkTickets + (size_t)kChunkMaxCtas * 4 + 255) / 256 * 256;   // 13312
 
 // Where each scratch region lives inside the caller's workspace.  All regions but the last depend
 // on the head counts and the batch only; the score bytes of the long-sequence scan come last and
@@ -28,7 +38,7 @@ inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
 struct WorkspaceLayout {
     size_t off_tickets;   // i32 [3][B][Hkv]  arrival counters of the split-K merge, then the two release counters per unit
-                          // of the pipelined step (first pass / second pass of SCORE + TOPK done); all zero between calls
+                          // of the pipelined step (first pass / second pass of SCORE + TOPK done); in front, zero between calls
     size_t off_hist;      // i32 [B][Hkv][kMaxChunks][33]   per-chunk score histograms
     size_t off_part_ml;   // f32 [slots][G][2]    split-K running max (log2 domain) and sum, slots = kMaxAttnCtas + B*Hkv
     size_t off_part_acc;  // f32 [slots][G][128]  split-K unnormalised outputs
@@ -45,8 +55,8 @@ inline size_t score_row_bytes(int max_seq_len) { return align_up((size_t)(max_se
 
 inline WorkspaceLayout make_layout(int B, int Hq, int Hkv, int max_seq_len) {
     WorkspaceLayout L;
-    size_t o = kHeaderBytes;
-    L.off_tickets = o;   o = align_up(o + (size_t)3 * B * Hkv * 4, 256);
+    size_t o = kWorkspaceFront;
+    L.off_tickets = kOffCounters;
     L.off_hist = o;      o = align_up(o + (size_t)B * Hkv * kMaxChunks * kBins * 4, 256);
     const size_t slots = (size_t)kMaxAttnCtas + (size_t)B * Hkv, G = (size_t)(Hq / (Hkv > 0 ? Hkv : 1));
     L.off_part_ml = o;   o = align_up(o + slots * G * 2 * 4, 256);

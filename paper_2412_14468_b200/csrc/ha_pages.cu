@@ -365,13 +365,13 @@ __global__ void __launch_bounds__(kP_Copy) pages_copy_kernel(const PageState p, 
     }
 }
 
-// ---- workspace: header, numbers, then the lists
+// ---- workspace: front, numbers, then the lists
 struct PagesLayout {
     size_t off_numbers, off_first, off_list, off_src, off_dst, total;
 };
 static PagesLayout pages_layout(int n_pages, int B) {
     PagesLayout L;
-    size_t o = kHeaderBytes;
+    size_t o = kWorkspaceFront;
     L.off_numbers = o; o += 256;
     L.off_first = o;   o = align_up(o + ((size_t)B + 1) * 4, 256);
     L.off_list = o;    o = align_up(o + (size_t)n_pages * 4, 256);

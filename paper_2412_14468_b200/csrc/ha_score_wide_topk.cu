@@ -573,14 +573,14 @@ static cudaError_t launch_wide_cluster(const WideArgs &a, int B, cudaStream_t st
     return cudaGetLastError();
 }
 
-// Workspace of the wide selection: header | unit histograms | chunk counts | 16-bit scores.
+// Workspace of the wide selection: front | unit histograms | chunk counts | 16-bit scores.
 struct WideLayout {
     size_t off_hist, off_counts, off_scores, score_row, total;
 };
 WideLayout wide_layout(int B, int Hkv, int max_seq_len) {
     WideLayout L;
     const size_t units = (size_t)B * Hkv;
-    size_t o = kHeaderBytes;
+    size_t o = kWorkspaceFront;
     L.off_hist = o;   o = align_up(o + units * kWideHistStride * 4, 256);
     L.off_counts = o; o = align_up(o + units * kWideMaxChunks * 2 * 4, 256);
     L.score_row = align_up((size_t)(max_seq_len > 0 ? max_seq_len : 0), 256);
