@@ -431,10 +431,14 @@ int ha_rotary_freqs(int32_t rot_dim, double theta, int32_t rule, double factor, 
  * tokens already, their pages are allocated): row i of n new ones is token seq_lens[b] - n + i, at that position, or at
  * positions[row] where positions is given.  A row whose token number is negative, or whose page lies outside 0 .. n_pages - 1
  * (HA_DEV_BAD_INDEX), is turned but not written to the cache.  Two new tokens must not share a slot (ha_pages_extend sees to it).
+ * Where ha_pages_extend makes the room, give both calls one workspace: behind a refused one, whose seq_lens do not count the new
+ * tokens, nothing is then written to the cache.
  *   q, k_new, v_new   bf16 rows [n_rows][heads][128] with strides as q of ha_chunk_attn_paged; q_out may be q
  *   k_out             bf16 [n_rows][n_kv_heads][128] contiguous or NULL: the turned keys once more, packed (for ha_encode_append_paged,
- *                     whose signatures belong to the keys as they are cached)
- *   workspace         may be NULL; else one with the library's header: its status word takes HA_DEV_BAD_INDEX */
+ *                     whose signatures belong to the keys as they are cached); behind a refused ha_pages_extend, the keys that lie
+ *                     where the new ones would have gone, so that the signatures there stay what they are
+ *   workspace         may be NULL; else one with the library's header: its status word takes HA_DEV_BAD_INDEX, and it tells of a
+ *                     refused ha_pages_extend */
 int ha_rotary_append_paged(const ha_shape *shape, const ha_tensor *q, const ha_tensor *k_new, const ha_tensor *v_new,
                            const ha_tensor *q_out, uint16_t *k_out, const int32_t *q_offsets, int32_t n_rows,
                            const double *inv_freq, int32_t rot_dim, const int32_t *positions, int32_t interleaved, float scale,
@@ -458,6 +462,10 @@ int ha_rotary_append_paged(const ha_shape *shape, const ha_tensor *q, const ha_t
  *                     own in its place, with K, V and signatures copied (every holder that grows in the call does).  All or
  *                     nothing: if the free pages do not suffice or a row would grow past max_pages, the call changes nothing and
  *                     raises HA_DEV_NO_PAGE; negative numbers or pages outside the pool: nothing, HA_DEV_BAD_INDEX.
+ *                     A captured loop does not look at the status between its calls: ha_rotary_append_paged with the same workspace
+ *                     leaves the cache alone until a later ha_pages_extend is granted (or ha_workspace_init), and the attention of
+ *                     the tokens that found no room is of no use.  (ha_sparse_decode_paged_host, which writes its tokens by itself, does
+ *                     not know of a refusal: ha_read_device_status in front of it tells.)
  *   ha_pages_free     the listed rows end: each of their pages has one holder less, seq_len becomes 0; the entries of the row stay
  *                     as they were.  A row listed again counts once.  A page that nobody holds raises HA_DEV_BAD_INDEX.
  *   ha_pages_compact  all pages in use move to numbers below their count n_used: those at or above it move, in ascending order, into

@@ -436,7 +436,8 @@ def ha_rotary_append_paged(shape: ha_shape, q, k_new, v_new, q_out, inv_freq, q_
                            seq_lens, workspace=None, k_out=None, positions=None, interleaved: bool = False, scale: float = 1.0,
                            stream=None) -> None:
     """New tokens into the paged cache: q bf16 [rows, Hq, 128] turned into q_out (may be q), k_new [rows, Hkv, 128] turned and written to
-    its pages (and to k_out), v_new written to its pages; rows packed by q_offsets, seq_lens count the new tokens already."""
+    its pages (and to k_out), v_new written to its pages; rows packed by q_offsets, seq_lens count the new tokens already.  workspace: the
+    one given to ha_pages_extend, behind whose refusal nothing is written to the cache."""
     _check("ha_rotary_append_paged", _host().rotary_append_paged(shape, q, k_new, v_new, q_out, inv_freq, q_offsets, K_pool, V_pool,
                                                                  block_table, page_size, seq_lens, workspace, k_out, positions,
                                                                  1 if interleaved else 0, scale, stream))

@@ -24,9 +24,10 @@ constexpr int kMaxUnits = 65536;       // (sequence, KV head) pairs
 // Workspaces.  A caller may give one workspace to calls of every kind and shape, one after the other, so every layout begins alike:
 // the header, then all counters that calls of one kind find at zero and leave at zero, whichever the kind; what any call leaves
 // behind otherwise lies further on.  ha_workspace_init clears that front.
-//   header     word 0: device status, 1 .. 7: the pipelined step
+//   header     word 0: device status, 1 .. 7: the pipelined step, 8: not 0 if the last ha_pages_extend was refused
 //   counters   i32 [3][units] of the decode step, units <= kMaxBalancedUnits: with more, no unit is cut and none is counted
 //   tickets    i32 [kChunkMaxCtas] of the attention of new tokens
+constexpr int kRefusedWord = 8;
 constexpr size_t kOffCounters = kHeaderBytes;
 constexpr size_t kOffChunkTickets = kOffCounters + (size_t)3 * kMaxBalancedUnits * 4;
 constexpr size_t kWorkspaceFront = (kOffChunkTickets + (size_t)kChunkMaxCtas * 4 + 255) / 256 * 256;   // 13312

@@ -185,12 +185,20 @@ __global__ void __launch_bounds__(kP_Plan, 1) pages_plan_extend_kernel(const Pag
         total += all;
         if (total > p.n_pages) wrong |= HA_DEV_NO_PAGE;
     }
+    // (the appends of the tokens that there is no room for learn of it: their places are other tokens' now)
+    auto refuse = [&](uint32_t bit) {
+        if (tid == 0) {
+            flag(p.status, bit);
+            p.status[kRefusedWord] = 1u;
+            plan.n_copies[0] = 0;
+        }
+    };
     if (__syncthreads_or((int)(wrong & HA_DEV_BAD_INDEX))) {
-        if (tid == 0) { flag(p.status, HA_DEV_BAD_INDEX); plan.n_copies[0] = 0; }
+        refuse(HA_DEV_BAD_INDEX);
         return;
     }
     if (__syncthreads_or((int)wrong)) {
-        if (tid == 0) { flag(p.status, HA_DEV_NO_PAGE); plan.n_copies[0] = 0; }
+        refuse(HA_DEV_NO_PAGE);
         return;
     }
     const int need = (int)total;
@@ -211,7 +219,7 @@ __global__ void __launch_bounds__(kP_Plan, 1) pages_plan_extend_kernel(const Pag
         found += all;
     }
     if (found < need) {                                // uniform
-        if (tid == 0) { flag(p.status, HA_DEV_NO_PAGE); plan.n_copies[0] = 0; }
+        refuse(HA_DEV_NO_PAGE);
         return;
     }
     __syncthreads();
@@ -238,7 +246,10 @@ __global__ void __launch_bounds__(kP_Plan, 1) pages_plan_extend_kernel(const Pag
     }
     __syncthreads();
     for (int b = tid; b < p.B; b += kP_Plan) p.seq_lens[b] = __ldcg(p.seq_lens + b) + __ldcg(n_new + b);
-    if (tid == 0) plan.n_copies[0] = s_copies;
+    if (tid == 0) {
+        plan.n_copies[0] = s_copies;
+        p.status[kRefusedWord] = 0u;
+    }
 }
 
 // ---- compact, first kernel: pages in use at or above their number U move into the holes below it, in order

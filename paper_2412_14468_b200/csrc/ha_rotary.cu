@@ -135,7 +135,11 @@ __global__ void __launch_bounds__(kR_Threads) rotary_kernel(const RotaryArgs a) 
 
     int pos;
     long long k_at = -1, v_at = -1;
+    // No room was made for the new tokens: the places that seq_lens gives them are those of tokens cached earlier, which stay.  k_out then
+    // holds those tokens' keys, so that a signature made of it is the one that is there.
+    bool refused = false;
     if (kAppend) {
+        refused = a.status && __ldcg(a.status + kRefusedWord) != 0u;
         const int b = sequence_of(a.offsets, a.B, row, lane);
         if (b < 0) return;
         const int o0 = __ldcg(a.offsets + b), o1 = __ldcg(a.offsets + b + 1);
@@ -176,11 +180,16 @@ __global__ void __launch_bounds__(kR_Threads) rotary_kernel(const RotaryArgs a) 
             const int g = h - a.heads;
             src = a.k + (long long)row * a.k_sn + (long long)g * a.k_sh;
             dst = k_at < 0 ? nullptr : const_cast<uint16_t *>(a.K.ptr) + k_at + (long long)g * a.K.sh;
+            if (refused && dst) {
+                src = dst;
+                dst = nullptr;
+                turn = false;
+            }
             if (a.k_out) also = a.k_out + ((long long)row * a.kv_heads + g) * kD;
         } else {
             const int g = h - a.heads - a.kv_heads;
             src = a.v + (long long)row * a.v_sn + (long long)g * a.v_sh;
-            dst = v_at < 0 ? nullptr : const_cast<uint16_t *>(a.V.ptr) + v_at + (long long)g * a.V.sh;
+            dst = v_at < 0 || refused ? nullptr : const_cast<uint16_t *>(a.V.ptr) + v_at + (long long)g * a.V.sh;
             turn = false;
         }
         uint4 va = __ldcg(reinterpret_cast<const uint4 *>(src + pa)), vb = __ldcg(reinterpret_cast<const uint4 *>(src + pb));
