@@ -378,8 +378,8 @@ int ha_sparse_decode_paged_codes(const ha_shape *shape, const ha_mapping *map_q,
  * are not written.  Tokens at or beyond seq_lens[b], and what lies in unused slots of a page, do not matter, NaN or not.
  *   q            bf16 rows [n_rows][n_q_heads][128]: stride_n steps over tokens, stride_h over heads (stride_b is not used; heads
  *                may overlap other data, as in one projection output that holds q, k and v), multiples of 8
- *   q_offsets    i32 [batch + 1], ascending, within 0 .. n_rows (device); a sequence with bad ones is left out and raises
- *                HA_DEV_BAD_INDEX
+ *   q_offsets    i32 [batch + 1], ascending, within 0 .. n_rows (device).  A sequence whose own two are not is left out and raises
+ *                HA_DEV_BAD_INDEX; a row that two sequences claim then is of no use
  *   K_pool, V_pool, block_table, page_size   as in ha_gather_attn_paged, except that the two pools' strides need not agree; n_pages
  *                bounds the page numbers: tokens on a page outside 0 .. n_pages - 1 read as zeros and raise HA_DEV_BAD_INDEX (the
  *                sequence's output is then of no use)

@@ -108,7 +108,7 @@ __device__ __forceinline__ void rotary_apply(const RotaryTurn &t, bool turns, co
     b = make_uint4(vb[0], vb[1], vb[2], vb[3]);
 }
 
-// The sequence that row belongs to: the last b with offsets[b] <= row; 32 offsets are looked at a time.  -1: none.
+// The last b with offsets[b] <= row, of ascending offsets; 32 offsets are looked at a time.  -1: none.
 __device__ __forceinline__ int sequence_of(const int32_t *offsets, int B, int row, int lane) {
     int lo = 0, n = B + 1;                // offsets[lo .. lo + n) are left, all in front of lo are <= row
     for (;;) {
@@ -124,6 +124,30 @@ __device__ __forceinline__ int sequence_of(const int32_t *offsets, int B, int ro
     }
 }
 
+__device__ __forceinline__ bool offsets_in_order(const int32_t *offsets, int b, int rows, int &o0, int &o1) {
+    o0 = __ldcg(offsets + b);
+    o1 = __ldcg(offsets + b + 1);
+    return o0 >= 0 && o1 >= o0 && o1 <= rows;
+}
+// The sequence that row belongs to, and its offsets; -1: none.  Where offsets are not ascending the search may miss the sequence that has
+// the row, so a row that it finds no place for is looked for in every sequence (as are the rows behind the last one: a load a lane for
+// every 32 sequences).
+__device__ __forceinline__ int owner_of(const int32_t *offsets, int B, int rows, int row, int lane, int &o0, int &o1) {
+    int b = sequence_of(offsets, B, row, lane);
+    if (b >= 0 && offsets_in_order(offsets, b, rows, o0, o1) && row >= o0 && row < o1) return b;
+    for (int b0 = 0; b0 < B; b0 += 32) {
+        b = b0 + lane;
+        const bool mine = b < B && offsets_in_order(offsets, b, rows, o0, o1) && row >= o0 && row < o1;
+        const uint32_t m = __ballot_sync(0xffffffffu, mine);
+        if (m) {
+            b = b0 + __ffs(m) - 1;
+            offsets_in_order(offsets, b, rows, o0, o1);
+            return b;
+        }
+    }
+    return -1;
+}
+
 template <bool kAppend>
 __global__ void __launch_bounds__(kR_Threads) rotary_kernel(const RotaryArgs a) {
     const int lane = threadIdx.x & 31, piece = lane & 7, group = lane >> 3;
@@ -131,6 +155,13 @@ __global__ void __launch_bounds__(kR_Threads) rotary_kernel(const RotaryArgs a) 
     const int row = (int)(unit / a.warps_per_row), part = (int)(unit % a.warps_per_row);
     pdl_wait();
     pdl_launch_dependents();   // no kernel reads what is written here before its own wait
+    if (kAppend && a.status && blockIdx.x == gridDim.x - 1) {   // a CTA behind those of the rows
+        int o0, o1;
+        bool bad = false;
+        for (int b = threadIdx.x; b < a.B; b += kR_Threads) bad |= !offsets_in_order(a.offsets, b, a.rows, o0, o1);
+        if (bad) atomicOr(a.status, HA_DEV_BAD_INDEX);
+        return;
+    }
     if (row >= a.rows) return;
 
     int pos;
@@ -140,13 +171,9 @@ __global__ void __launch_bounds__(kR_Threads) rotary_kernel(const RotaryArgs a) 
     bool refused = false;
     if (kAppend) {
         refused = a.status && __ldcg(a.status + kRefusedWord) != 0u;
-        const int b = sequence_of(a.offsets, a.B, row, lane);
-        if (b < 0) return;
-        const int o0 = __ldcg(a.offsets + b), o1 = __ldcg(a.offsets + b + 1);
-        if (o0 < 0 || o1 > a.rows || row >= o1) {   // rows of no sequence; offsets that are not ascending or leave the rows
-            if (a.status && (o0 < 0 || o1 > a.rows || o1 < o0) && lane == 0) atomicOr(a.status, HA_DEV_BAD_INDEX);
-            return;
-        }
+        int o0, o1;
+        const int b = owner_of(a.offsets, a.B, a.rows, row, lane, o0, o1);
+        if (b < 0) return;                // of no sequence
         const int tok = __ldcg(a.seq_lens + b) - o1 + row;
         pos = a.positions ? __ldcg(a.positions + row) : tok;
         if (tok >= 0) {
@@ -217,7 +244,7 @@ static int rotary_warps_per_row(int rows, int heads) {
 template <bool kAppend>
 static cudaError_t launch_rotary_kernel(const RotaryArgs &a, int heads, cudaStream_t st) {
     const long long warps = (long long)a.rows * a.warps_per_row;
-    const dim3 grid((unsigned)((warps * 32 + kR_Threads - 1) / kR_Threads));
+    const dim3 grid((unsigned)((warps * 32 + kR_Threads - 1) / kR_Threads) + (kAppend && a.status ? 1u : 0u));
     const cudaError_t e = launch_pdl(rotary_kernel<kAppend>, grid, dim3(kR_Threads), 0, st, a);
     if (e != cudaSuccess) return e;
     count_launch();
