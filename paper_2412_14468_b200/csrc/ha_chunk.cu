@@ -39,7 +39,6 @@
 
 #include <cstring>
 #include <type_traits>
-#include <cuda.h>   // CUtensorMap (types only; the encoder is fetched through the runtime)
 
 namespace ha {
 
@@ -945,19 +944,6 @@ size_t chunk_workspace_bytes() {
 
 // Tensor maps (bf16, strides in elements): q [n_rows][Hq][128] and a pool [n_pages][Hkv][page][128], both with the 128 columns as two
 // halves of 64; false if the driver's encoder is missing or the strides do not fit a tensor map.
-typedef CUresult (*EncodeTiled)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
-                                const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-static EncodeTiled encode_tiled() {
-    static const EncodeTiled fn = [] {
-        void *p = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess && q == cudaDriverEntryPointSuccess)
-            return reinterpret_cast<EncodeTiled>(p);
-        cudaGetLastError();
-        return (EncodeTiled) nullptr;
-    }();
-    return fn;
-}
 static bool encode_map(CUtensorMap *tm, int rank, const void *base, const cuuint64_t *dims, const cuuint64_t *strides, const cuuint32_t *box) {
     const cuuint32_t step[5] = {1u, 1u, 1u, 1u, 1u};
     const EncodeTiled fn = encode_tiled();

@@ -21,7 +21,6 @@
 
 #include <cstring>
 #include <type_traits>
-#include <cuda.h>   // CUtensorMap (types only; the encoder is fetched through the runtime)
 
 namespace ha {
 
@@ -609,24 +608,22 @@ __global__ void __launch_bounds__(kU_Threads, 1) encode_umma_kernel(const __grid
     }
 }
 
+EncodeTiled encode_tiled() {
+    static const EncodeTiled fn = [] {
+        void *p = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess && q == cudaDriverEntryPointSuccess)
+            return reinterpret_cast<EncodeTiled>(p);
+        cudaGetLastError();
+        return (EncodeTiled) nullptr;
+    }();
+    return fn;
+}
+
 // Tensor map of x [B][H][T][128] (bf16, strides in elements) seen as [B][H][2][T][64], with boxes of
 // 64 x 128 x 2 elements; false if the driver entry point is missing or the strides do not fit a tensor map.
 static bool make_x_tensor_map(CUtensorMap *tm, TensorView x, int B, int H, int T) {
-    typedef CUresult (*EncodeFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
-                                 const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-    static EncodeFn fn = nullptr;
-    static bool looked = false;
-    if (!looked) {
-        void *p = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess &&
-            q == cudaDriverEntryPointSuccess)
-            fn = reinterpret_cast<EncodeFn>(p);
-        else
-            cudaGetLastError();
-        looked = true;
-    }
+    const EncodeTiled fn = encode_tiled();
     if (!fn) return false;
     const cuuint64_t dims[5] = {64u, (cuuint64_t)T, 2u, (cuuint64_t)H, (cuuint64_t)B};
     const cuuint64_t strides[4] = {(cuuint64_t)x.sn * 2, 128u, (cuuint64_t)x.sh * 2, (cuuint64_t)x.sb * 2};   // bytes

@@ -1,9 +1,16 @@
-// Fifth-generation tensor cores: descriptors, issue, tensor-memory access (included by ha_encode_tc.cu and ha_chunk.cu).
+// Fifth-generation tensor cores: descriptors, issue, tensor-memory access, and the encoder of tensor maps (included by ha_encode_tc.cu and ha_chunk.cu).
 #pragma once
 
 #include "ha_common.cuh"
 
+#include <cuda.h>   // CUtensorMap (types only; the encoder is fetched through the runtime)
+
 namespace ha {
+
+// The driver's encoder of tensor maps, looked up once for the process, whichever threads ask first; NULL if it is missing.
+typedef CUresult (*EncodeTiled)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
+                                const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiled encode_tiled();   // (ha_encode_tc.cu)
 
 // 64-bit shared-memory matrix descriptor, no swizzle: start address, leading and stride byte offsets
 // in 16-byte units, descriptor version 1 (bits 46-47), layout type 0 (bits 61-63).

@@ -3,6 +3,7 @@
 #include <atomic>
 #include <chrono>
 #include <cstring>
+#include <mutex>
 #include <thread>
 
 #include <cuda_runtime_api.h>
@@ -19,6 +20,7 @@ struct Watch { std::string text; int arg, words; };
 static std::vector<Watch> watches;
 static std::vector<std::vector<unsigned long long>> seen;
 static std::atomic<int> lookups{0};
+static std::mutex one_at_a_time;
 
 static void look(const void *f, void **args) {
     for (const Watch &w : watches)
@@ -30,10 +32,12 @@ static void look(const void *f, void **args) {
 }
 extern "C" {
 cudaError_t cudaLaunchKernelExC(const cudaLaunchConfig_t *c, const void *f, void **args) {
+    std::lock_guard<std::mutex> lock(one_at_a_time);
     look(f, args);
     return launch_by_name(c, f, args);
 }
 cudaError_t cudaLaunchKernel(const void *f, dim3 g, dim3 b, void **args, size_t s, cudaStream_t st) {
+    std::lock_guard<std::mutex> lock(one_at_a_time);
     look(f, args);
     return launch_plain_by_name(f, g, b, args, s, st);
 }
