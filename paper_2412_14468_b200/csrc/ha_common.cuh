@@ -91,12 +91,14 @@ inline int chunk_tokens_for(int n_units, int max_seq_len, int n_sm) {
 
 // ---- programmatic dependent launch: a kernel launched with launch_pdl may start while its
 // predecessor in the stream is still running; everything it reads from, or writes over, earlier
-// work must come after pdl_wait().  Three rules make the exceptions sound:
+// work must come after pdl_wait().  Four rules make the exceptions sound:
 //  * before the wait only mapping networks, sequence lengths, budgets and contiguous 32-bit signatures are read (inside a
 //    layer-step, behind its ENCODE, paged ones and the block table too);
 //  * a kernel that writes signatures releases its dependents when they are written.  The ENCODE of a layer-step releases
 //    early: its SCORE reads the appended token again, and GATHER-ATT releases the next call behind its own wait.
 //    ha_encode_wide does too: the wide selection reads no signature before its wait;
+//  * a kernel that writes sequence lengths (ha_pages.cu) never releases its dependents, and its CTAs end when their lengths can be
+//    read: they are written by a kernel that another of the call has waited for, or a fence stands behind them;
 //  * at least one CTA of every grid waits, so that a wait reaches back through everything older in the stream.
 #ifdef __CUDACC__
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }

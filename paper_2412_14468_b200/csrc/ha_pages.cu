@@ -10,7 +10,7 @@
 // bound by HBM.  Measured: fork, extend (two launches) and free of four children of 4099 tokens 17 us, of 128 children with their
 // copies 27; compaction of 27 900 pages of 16 tokens, 11 500 of them moved, 290 us (5.2 TB/s; 4, 8 pieces of a thread in flight and
 // 8, 16 CTAs a SM: 290, 361, 306).  None of them lets the kernels behind it start early: they write sequence lengths, which others
-// read before their own wait.
+// read before their own wait (the rules are in ha_common.cuh).
 #include "ha_common.cuh"
 
 namespace ha {
@@ -72,7 +72,10 @@ __global__ void __launch_bounds__(kP_Threads) pages_fork_kernel(const PageState 
         if ((unsigned)page < (unsigned)p.n_pages) atomicAdd(p.ref + page, 1);
         else flag(p.status, HA_DEV_BAD_INDEX);
     }
-    if (threadIdx.x == 0) p.seq_lens[child] = len;     // every thread has read it: behind the barrier above
+    if (threadIdx.x == 0) {                            // every thread has read it: behind the barrier above
+        p.seq_lens[child] = len;
+        __threadfence();                               // kernels behind read it before their wait
+    }
 }
 
 // ---- free: every page of the sequence counts one holder less
@@ -102,7 +105,10 @@ __global__ void __launch_bounds__(kP_Threads) pages_free_kernel(const PageState 
         if (!ok) flag(p.status, HA_DEV_BAD_INDEX);
     }
     __syncthreads();
-    if (threadIdx.x == 0) p.seq_lens[seq] = 0;
+    if (threadIdx.x == 0) {
+        p.seq_lens[seq] = 0;
+        __threadfence();                               // kernels behind read it before their wait
+    }
 }
 
 // exclusive sum over the CTA and the whole sum
