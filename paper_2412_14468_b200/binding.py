@@ -423,9 +423,12 @@ def ha_rotary(x, out, inv_freq, positions, interleaved: bool = False, inverse: b
     _check("ha_rotary", _host().rotary(x, out, inv_freq, positions, 1 if interleaved else 0, 1 if inverse else 0, scale, stream))
 
 
-def ha_rotary_freqs(rot_dim: int, theta: float, rule: int = HA_ROTARY_PLAIN, factor: float = 1.0, low: float = 1.0, high: float = 4.0,
-                    original_context: float = 8192.0):
-    """(inv_freq float64 [rot_dim / 2] on the CPU, scale) by one of the HA_ROTARY_* rules."""
+def ha_rotary_freqs(rot_dim: int, theta: float, rule: int = HA_ROTARY_PLAIN, factor: float = 1.0, low: float = 1.0,
+                    high: Optional[float] = None, original_context: float = 8192.0):
+    """(inv_freq float64 [rot_dim / 2] on the CPU, scale) by one of the HA_ROTARY_* rules; high: by default the rule's own, 32 for
+    HA_ROTARY_YARN, 4 for HA_ROTARY_BANDS."""
+    if high is None:
+        high = 32.0 if rule == HA_ROTARY_YARN else 4.0
     freq = torch.empty(max(0, rot_dim // 2), dtype=torch.float64)
     scale = C.c_float(1.0)
     _check("ha_rotary_freqs", lib().ha_rotary_freqs(rot_dim, theta, rule, factor, low, high, original_context, freq.data_ptr(), C.byref(scale)))
