@@ -59,7 +59,7 @@ extern "C" {
 #define HA_ERR_STATIC_LIMIT 5 /* ha_gather_attn_static: problem larger than the library's built-in scratch */
 
 /* bits of the device status word (ha_read_device_status) */
-#define HA_DEV_BAD_INDEX 1u /* an idx entry >= seq_len was met and skipped */
+#define HA_DEV_BAD_INDEX 1u /* an idx entry >= seq_len was met and skipped; a page, offset or sequence that a call names is a bad one */
 #define HA_DEV_TIMEOUT 2u   /* a bounded wait inside a kernel gave up (ha_encode_prefill's tensor-core path,
                                ha_sparse_decode_pipelined, ha_chunk_attn_paged); the kernel returned early and its outputs are not valid */
 
@@ -385,9 +385,10 @@ int ha_sparse_decode_paged_codes(const ha_shape *shape, const ha_mapping *map_q,
  *                sequence's output is then of no use)
  *   out          bf16 [n_rows][n_q_heads][128] contiguous, apart from q; lse fp32 [n_rows][n_q_heads] or NULL
  *   workspace    ha_workspace_bytes_chunk() bytes, the same for all shapes; prepared once with ha_workspace_init
- * n_sink / n_local of the shape are not looked at.  Results do not depend on how the work is split: the same call gives the same
- * bits.  If a wait inside the kernel runs out (it never should) it raises HA_DEV_TIMEOUT and out must not be used; call
- * ha_workspace_init before the workspace is used again. */
+ * n_sink / n_local of the shape are not looked at.  The same call gives the same bits.  Where a sequence's keys are cut between SMs
+ * goes by the whole batch, so with other sequences beside it its results may differ in their roundings.  Sequences that bring no rows
+ * cost about 0.2 us each where they lie behind one that does (an SM passes over them one by one).  If a wait inside the kernel runs out
+ * (it never should) it raises HA_DEV_TIMEOUT and out must not be used; call ha_workspace_init before the workspace is used again. */
 size_t ha_workspace_bytes_chunk(void);
 int ha_chunk_attn_paged(const ha_shape *shape, const ha_tensor *q, const int32_t *q_offsets, int32_t n_rows,
                         const ha_tensor *K_pool, const ha_tensor *V_pool, int32_t n_pages, const int32_t *block_table,
@@ -455,8 +456,8 @@ int ha_rotary_append_paged(const ha_shape *shape, const ha_tensor *q, const ha_t
  *
  *   ha_pages_fork     row children[i] becomes a copy of row parents[i] (i = 0 .. n_forks - 1): same length, same pages, each with
  *                     one holder more.  Nothing is copied until ha_pages_extend writes into a shared page.  A fork whose child is in
- *                     use (seq_len != 0), was listed before, or is a parent in the same call, or whose numbers lie outside the
- *                     batch, is left out and raises HA_DEV_BAD_INDEX.  One parent may have many children.
+ *                     use (seq_len != 0) or was listed before, whose parent is listed as a child in the same call, or whose
+ *                     numbers lie outside the batch, is left out and raises HA_DEV_BAD_INDEX.  One parent may have many children.
  *   ha_pages_extend   room for n_new[b] >= 0 tokens behind each sequence: new pages are entered in its row, and seq_lens[b] grows by
  *                     n_new[b].  A sequence that grows and whose last page is partly filled and has other holders gets a page of its
  *                     own in its place, with K, V and signatures copied (every holder that grows in the call does).  All or

@@ -7,7 +7,8 @@
 //
 // What bounds these: pages_fork and pages_free are a launch and two dependent loads; pages_plan_* read the reference counts with one
 // CTA of 1024 threads (16 counts a thread and round, all loads of a round in flight); pages_copy_kernel moves whole pages and is
-// bound by HBM.  Measured: fork, extend (two launches) and free of four children of 4099 tokens 17 us, of 128 children with their
+// bound by HBM where there are many (an extend has a CTA for a sequence and KV head, whatever the page size: one copy of 1024 tokens
+// and 8 heads takes 78 us, 0.1 TB/s).  Measured: fork, extend (two launches) and free of four children of 4099 tokens 17 us, of 128 children with their
 // copies 27; compaction of 27 900 pages of 16 tokens, 11 500 of them moved, 290 us (5.2 TB/s; 4, 8 pieces of a thread in flight and
 // 8, 16 CTAs a SM: 290, 361, 306).  None of them lets the kernels behind it start early: they write sequence lengths, which others
 // read before their own wait (the rules are in ha_common.cuh).
