@@ -230,9 +230,9 @@ __device__ __forceinline__ void chunk_fetch(const ChunkArgs &a, NextPart next_pa
     auto look_up = [&](int j) {
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
-            const int tok = j * kChunkTile + g * 32 + lane;
+            const uint32_t tok = (uint32_t)j * kChunkTile + g * 32 + lane;   // a last tile may end behind 2^31
             row_pages[g] = -1;
-            if (tok < now.n) {
+            if (tok < (uint32_t)now.n) {
                 row_pages[g] = __ldcg(a.table + (long long)now.b * a.bt_sb + (tok >> a.shift));
                 if (bad_page(row_pages[g])) row_pages[g] = -1;
             }
@@ -245,7 +245,7 @@ __device__ __forceinline__ void chunk_fetch(const ChunkArgs &a, NextPart next_pa
             for (int i = 0; i < 16; ++i) {
                 const int r = g * 32 + 2 * i + hw, page = __shfl_sync(0xffffffffu, row_pages[g], 2 * i + hw);
                 const uint16_t *src = T.ptr + ch * 8;
-                if (page >= 0) src += (long long)page * T.sb + (long long)now.h * T.sh + (long long)((j * kChunkTile + r) & mask) * T.sn;
+                if (page >= 0) src += (long long)page * T.sb + (long long)now.h * T.sh + (long long)(((uint32_t)j * kChunkTile + r) & mask) * T.sn;
                 const uint32_t at = kV ? ((uint32_t)(r >> lbox) << lbox) * 256 + (uint32_t)(ch >> 3) * (128u << lbox) + (uint32_t)(r & ((1 << lbox) - 1)) * 128
                                        : (uint32_t)(ch >> 3) * kC_Half + (uint32_t)r * 128;
                 cp_async16(dst + at + (((ch & 7) ^ (r & 7)) << 4), src, page >= 0 ? 16u : 0u);
@@ -272,7 +272,8 @@ __device__ __forceinline__ void chunk_fetch(const ChunkArgs &a, NextPart next_pa
             by_tma = false;
         } else {
             // a lane for each box; boxes behind the end of the sequence are left out (their keys are masked, whatever they are)
-            const int which = lane & ((1 << lboxes) - 1), half = lane >> lboxes, tok = j * kChunkTile + (which << lbox);
+            const int which = lane & ((1 << lboxes) - 1), half = lane >> lboxes;
+            const uint32_t tok = (uint32_t)j * kChunkTile + ((uint32_t)which << lbox);
             const int batch = (j * kChunkTile >> a.shift) >> 5;
             const int page = __shfl_sync(0xffffffffu, batch & 1 ? pages1 : pages0, (tok >> a.shift) & 31);
             const int left = now.n - j * kChunkTile, there = left >= kChunkTile ? 1 << lboxes : (left + (1 << lbox) - 1) >> lbox;
@@ -764,7 +765,7 @@ __global__ void __launch_bounds__(kC_Threads, 1) chunk_attn_kernel(const __grid_
                         if (!mine) continue;
                         if (now.wild_v) {              // what was taken out of the V tiles, for the tokens that this row sees
                             const int first = now.first_pos + 1 > 0 ? (now.first_pos + 1) & ~(kChunkTile - 1) : 0, lo = t0 * kChunkTile;
-                            const int end = limit < t1 * kChunkTile ? limit : t1 * kChunkTile;
+                            const int end = (uint32_t)limit < (uint32_t)t1 * kChunkTile ? limit : t1 * kChunkTile;
                             for (int tok = first > lo ? first : lo; tok < end; ++tok) {
                                 const int page = __ldcg(a.table + (long long)now.b * a.bt_sb + (tok >> a.shift));
                                 if ((unsigned)page >= (unsigned)a.n_pages) continue;

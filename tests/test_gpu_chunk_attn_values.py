@@ -91,3 +91,31 @@ def test_rows_that_are_not_in_use(ws, rows_of_the_table, where):
     c.run(ws)
     torch.cuda.synchronize()
     c.check(ws)
+
+
+def test_as_many_tokens_as_a_length_can_count(ws):
+    """2^31 - 1 tokens, all on one page of 65536: the last tile ends behind 2^31.
+
+    The terms have one sign, and each addition in 32 bits is off by at most 2^-23 (cut off, not rounded) of what has been added up.  One
+    half of an SM takes at most 2^24 / 148 / 2 + 2 key tiles.  A row's sum is added to once a tile; its output eight times, as the product
+    with V is eight instructions of 16 tokens, each of which adds to the accumulator."""
+    n, page = 2 ** 31 - 1, 65536
+    g = torch.Generator(DEV).manual_seed(3)
+    K = torch.randn(1, 1, page, 128, device=DEV, generator=g).to(torch.bfloat16)
+    V = torch.rand(1, 1, page, 128, device=DEV, generator=g).to(torch.bfloat16)
+    q = torch.randn(1, 1, 128, device=DEV, generator=g).to(torch.bfloat16)
+    ints = lambda v: torch.tensor(v, dtype=torch.int32, device=DEV)  # noqa: E731
+    table = torch.zeros(1, 2 ** 31 // page, dtype=torch.int32, device=DEV)
+    out, lse = torch.empty_like(q), torch.empty(1, 1, device=DEV)
+    ha.ha_chunk_attn_paged(ha.make_shape(1, 1, 1, 128 ** -0.5), q, ints([0, 1]), K, V, table, page, ints([n]), out, ws, lse=lse)
+    torch.cuda.synchronize()
+    assert ha.ha_read_device_status(ws) == 0
+    times = torch.full((page,), 2.0 ** 31 / page, dtype=torch.float64, device=DEV)
+    times[-1] -= 1
+    s = K[0, 0].double() @ q[0, 0].double() * 128 ** -0.5
+    w = times * torch.exp(s - s.max())
+    want = (w @ V[0, 0].double()) / w.sum()
+    sums = (2 ** 24 / 148 / 2 + 2) * 2 ** -23
+    off = (out[0, 0].double() - want).abs()
+    assert bool((off <= 2 ** -8 * want + (1 + 2 ** -8) * (2 ** -8 + 2 ** -12 + (8 + 1) * sums) * want).all()), float((off / want).max())
+    assert abs(float(lse) - float(s.max() + torch.log(w.sum()))) <= 2 ** -12 + sums
